@@ -313,6 +313,91 @@ int slapo_colreduce_partials(int dtype, int64_t nblk, int64_t stride, int64_t N,
  * draw >= round(p * 65536). */
 int slapo_dropout_mask(const slapo_layer_desc *desc, int site, int64_t T, uint8_t *mask, void *stream);
 
+/* ---- operators beside the layers ---------------------------------------------------------------------
+ * What the training of an encoder-decoder pair (or of a decoder that reads the states of an image or video encoder) needs next
+ * to its layers: attention to states of another length, rotary positions of several axes, and the norm of all gradients with
+ * their clipping. The conventions at the top hold here too. */
+
+/* Cross attention: every query token of a sample attends to the states (keys and values) of another sequence.
+ *   s_ij = scale q_i.k_j over the visible states j < kv_lens[b];  lse_i = log sum_j exp s_ij;  out_i = sum_j exp(s_ij - lse_i) v_j
+ * Tokens are rows with their heads side by side, head a in columns a*head_dim .. of q and out, key head c in columns c*head_dim .. of
+ * k and v. heads / kv_heads consecutive query heads share a key head (kv_heads = heads: each has its own). The strides are elements from one
+ * token to the next (0: packed, heads * head_dim or kv_heads * head_dim), so q may be part of a wider projection, and keys and
+ * values the halves of one (v = k + kv_heads * head_dim, kv_stride = 2 * kv_heads * head_dim) or of the projections of several
+ * decoder layers side by side; samples follow each other, len * stride apart. Columns between the rows are left alone.
+ * Sizes: head_dim 64 or 128; heads a multiple of kv_heads; strides multiples of 8; of each array a sample (and 256 tokens more) below 2^31
+ * bytes; batch and heads at most 65535; q_len * heads / kv_heads below 2^30. */
+typedef struct {
+  int32_t batch, q_len, kv_len, heads, kv_heads, head_dim;
+  int32_t dtype;                            /* SLAPO_BF16 | SLAPO_FP32 | SLAPO_FP16: q, k, v, out and their gradients */
+  float scale;                              /* of the scores, finite and >= 0; 0: 1 / sqrt(head_dim) */
+  int64_t q_stride, kv_stride, out_stride;  /* of q and dq; k, v, dk and dv; out and dout */
+} slapo_cross_attn_desc;
+
+/* Bytes of device workspace that forward and backward of this shape need (forward: may be 0, ws may then be NULL). A workspace serves
+ * one call at a time and is free again when the call's work is done. */
+int slapo_cross_attn_workspace(const slapo_cross_attn_desc *desc, size_t *fwd_bytes, size_t *bwd_bytes);
+
+/* kv_lens: device int32 [batch], visible states of each sample (values outside 0 .. kv_len count as the nearer end), or NULL: all.
+ * What lies in the states behind them, infinities and NaN included, reaches no result. Where a sample has none, out is 0 and lse -infinity.
+ * lse: fp32 [batch, heads, q_len] (natural log), which backward needs; may be NULL. out overlaps no input. */
+int slapo_cross_attn_fwd(const slapo_cross_attn_desc *desc, const void *q, const void *k, const void *v, const int32_t *kv_lens,
+                         void *out, float *lse, void *ws, void *stream);
+
+/* Backward: dq, dk and dv from dout = dL/dout, the inputs, and the out and lse of the matching forward. dk and dv are summed over the query
+ * heads that share a key head; those of hidden states, and all gradients of a sample without states, are 0. The gradients overlap neither
+ * each other nor the inputs. */
+int slapo_cross_attn_bwd(const slapo_cross_attn_desc *desc, const void *q, const void *k, const void *v, const int32_t *kv_lens,
+                         const void *out, const void *dout, const float *lse, void *dq, void *dk, void *dv, void *ws, void *stream);
+
+/* Rotary embedding with positions of several axes (time, height and width of video tokens, rows and columns of an image's patches),
+ * on the first `heads` heads of every row: queries and keys of a packed projection, or either of them alone. The pairs (2j, 2j+1) of a
+ * head are dealt out to the axes in order, pairs[a] to axis a; those that are left over are not turned. Pair j, the i-th of axis a, is
+ * turned by positions[row][a] * base^(-2j/head_dim) (SLAPO_ROPE_SHARED) or base^(-i/pairs[a]) (SLAPO_ROPE_PER_AXIS).
+ * With one axis of head_dim / 2 pairs and positions counted from 0 in every sequence this is slapo_rope.
+ * Sizes: head_dim a multiple of 8 up to 256, 1 to 4 axes, rows below 2^31, strides (elements from one row to the next; 0: heads * head_dim)
+ * multiples of 8 below 2^28. */
+enum { SLAPO_ROPE_SHARED = 0, SLAPO_ROPE_PER_AXIS = 1 };
+typedef struct {
+  int64_t rows;
+  int32_t heads, head_dim, axes;
+  int32_t pairs[4];
+  int32_t ladder;                           /* SLAPO_ROPE_SHARED | SLAPO_ROPE_PER_AXIS */
+  float base;                               /* of the frequencies, > 1 */
+  int32_t dtype;                            /* SLAPO_BF16 | SLAPO_FP32 | SLAPO_FP16 */
+  int64_t in_stride, out_stride;
+} slapo_rope_axes_desc;
+/* positions: device int32 [rows, axes], any values (angles are taken in 64 bits). out may be the array `in` itself (with the same
+ * stride), else they share no memory (SLAPO_ERR_SHAPE); columns behind the heads are neither read nor written. inverse != 0 turns by the
+ * negative angles: the transpose, which maps gradients w.r.t. rotated vectors back. */
+int slapo_rope_axes(const slapo_rope_axes_desc *desc, const int32_t *positions, const void *in, void *out, int inverse, void *stream);
+
+/* The 2-norm of many gradient arrays taken together, and their clipping to a bound on it: out = grad * min(1, max_norm / norm).
+ * An array: `count` elements (0: none, its pointers are not looked at) at `grad`, 16-byte aligned; the clipped values go to `out`, or back to
+ * `grad` if out is NULL or equals it. An array that is written shares memory with no other (SLAPO_ERR_SHAPE). */
+typedef struct {
+  const void *grad;
+  void *out;
+  int64_t count;
+  int32_t dtype;                            /* of both; may differ from array to array */
+} slapo_grad;
+/* A plan holds which arrays take part. slapo_grad_plan_bytes says how much device memory it needs; slapo_grad_plan_build enqueues its
+ * construction in `memory` (16-byte aligned) on `stream` and fills the host struct. The plan stays valid, for any values in the arrays, while the
+ * arrays and the memory stay where they are, and serves one call at a time (its memory also holds partial sums). n = 0 is
+ * accepted: the sum is 0. SLAPO_ERR_WORKSPACE: no host memory for the check. */
+typedef struct {
+  void *memory;
+  int64_t n, segments, segment;
+} slapo_grad_plan;
+int slapo_grad_plan_bytes(int32_t n, const slapo_grad *grads, size_t *bytes);
+int slapo_grad_plan_build(int32_t n, const slapo_grad *grads, void *memory, slapo_grad_plan *plan, void *stream);
+/* sumsq: device, one double: (accumulate ? *sumsq : 0) + the sum of squares of all arrays' elements, taken and added in 64 bits in an order
+ * that the plan fixes. Ranks that hold parts of one model add up theirs (the caller's all-reduce) between the two calls. */
+int slapo_grad_sumsq(const slapo_grad_plan *plan, int accumulate, double *sumsq, void *stream);
+/* norm = sqrt(*sumsq), written to `norm` (device, one float; may be NULL). Where it is at most max_norm (> 0; infinity clips nothing),
+ * or infinite or no number (the caller skips such a step), `out` gets the gradients as they are, else scaled by max_norm / norm. */
+int slapo_grad_clip(const slapo_grad_plan *plan, const double *sumsq, float max_norm, float *norm, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,6 +15,7 @@ GELU, RELU = 0, 1
 NT, NN, TN = 0, 1, 2
 EPI_NONE, EPI_BIAS, EPI_BIAS_ACT, EPI_DACT, EPI_ADD, EPI_GATE, EPI_DGATE = 0, 1, 2, 3, 4, 5, 6
 CLASSIC, LLAMA = 0, 1
+ROPE_SHARED, ROPE_PER_AXIS = 0, 1
 PARAM_NAMES = ("wqkv", "bqkv", "wo", "bo", "ln1_g", "ln1_b", "w1", "b1", "w2", "b2", "ln2_g", "ln2_b")
 
 
@@ -28,6 +29,25 @@ class LayerDesc(C.Structure):
 
 class _Ptrs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in PARAM_NAMES]
+
+
+class CrossAttnDesc(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_len", C.c_int32), ("kv_len", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("q_stride", C.c_int64), ("kv_stride", C.c_int64),
+                ("out_stride", C.c_int64)]
+
+
+class RopeAxesDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("heads", C.c_int32), ("head_dim", C.c_int32), ("axes", C.c_int32), ("pairs", C.c_int32 * 4),
+                ("ladder", C.c_int32), ("base", C.c_float), ("dtype", C.c_int32), ("in_stride", C.c_int64), ("out_stride", C.c_int64)]
+
+
+class _Grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
+
+
+class _GradPlan(C.Structure):
+    _fields_ = [("memory", C.c_void_p), ("n", C.c_int64), ("segments", C.c_int64), ("segment", C.c_int64)]
 
 
 class SlapoError(RuntimeError):
@@ -75,6 +95,14 @@ def lib():
             "slapo_weight_grad_workspace": [i32, i64, i64, i64, C.POINTER(C.c_size_t)],
             "slapo_weight_grad": [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp],
             "slapo_weight_grad_static": [i32, i32, i64, i64, i64, vp, vp, vp, vp],
+            "slapo_cross_attn_workspace": [C.POINTER(CrossAttnDesc), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+            "slapo_cross_attn_fwd": [C.POINTER(CrossAttnDesc), vp, vp, vp, vp, vp, vp, vp, vp],
+            "slapo_cross_attn_bwd": [C.POINTER(CrossAttnDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp],
+            "slapo_rope_axes": [C.POINTER(RopeAxesDesc), vp, vp, vp, i32, vp],
+            "slapo_grad_plan_bytes": [i32, C.POINTER(_Grad), C.POINTER(C.c_size_t)],
+            "slapo_grad_plan_build": [i32, C.POINTER(_Grad), vp, C.POINTER(_GradPlan), vp],
+            "slapo_grad_sumsq": [C.POINTER(_GradPlan), i32, vp, vp],
+            "slapo_grad_clip": [C.POINTER(_GradPlan), vp, C.c_float, vp, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -267,6 +295,181 @@ def slapo_rope(desc, qkv, table, inverse=0, stream=None):
     _check(lib().slapo_rope(C.byref(desc), _p(qkv), _p(table), inverse, _stream(stream)), "slapo_rope")
 
 
+# ---- operators beside the layers. Their tensors may be views, so each is checked against the descriptor before its address is taken:
+# its type, its extent, where it lies. (A wrong one would be read or written out of bounds, which the library cannot see.)
+_TORCH = {BF16: torch.bfloat16, FP32: torch.float32, FP16: torch.float16}
+_DTYPE = {v: k for k, v in _TORCH.items()}
+
+
+def _refuse(name, t, want):
+    raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {t.dtype}, on {t.device}: {want} is wanted on the stream's device")
+
+
+def _arg(name, t, dtype, shape, strides, device, optional=False):
+    """Address of a tensor of exactly this kind."""
+    if t is None and optional:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.device.index != device or not t.is_cuda or t.stride() != strides:
+        # (the stride of a dimension of one element says nothing)
+        if t.dtype is dtype and t.shape == shape and t.is_cuda and t.device.index == device and \
+                all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), strides)):
+            return t.data_ptr()
+        _refuse(name, t, f"{dtype} of shape {tuple(shape)} with strides {tuple(strides)}")
+    return t.data_ptr()
+
+
+def _room(name, t, nbytes, device):
+    """Address of a workspace."""
+    if t is None:
+        if nbytes:
+            raise ValueError(f"{name}: a workspace of {nbytes} bytes is wanted")
+        return None
+    if not t.is_cuda or t.device.index != device or not t.is_contiguous() or t.numel() * t.element_size() < nbytes:
+        _refuse(name, t, f"{nbytes} contiguous bytes")
+    return t.data_ptr()
+
+
+def _stream_and_device(stream):
+    s = stream if stream is not None else torch.cuda.current_stream()
+    if s.device_index != torch.cuda.current_device():   # (kernels are launched on the current device)
+        raise ValueError(f"the stream belongs to device {s.device_index}, the current device is {torch.cuda.current_device()}")
+    return s.cuda_stream, s.device_index
+
+
+def make_cross_attn_desc(**kw) -> CrossAttnDesc:
+    """kv_heads defaults to heads, the strides to packed rows, scale to 1 / sqrt(head_dim)."""
+    vals = dict(batch=1, q_len=1, kv_len=1, heads=1, kv_heads=kw.get("heads", 1), head_dim=64, dtype=BF16, scale=0.0, q_stride=0,
+                kv_stride=0, out_stride=0)
+    vals.update(kw)
+    return CrossAttnDesc(**vals)
+
+
+def slapo_cross_attn_workspace(desc: CrossAttnDesc):
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().slapo_cross_attn_workspace(C.byref(desc), C.byref(a), C.byref(b)), "slapo_cross_attn_workspace")
+    return a.value, b.value
+
+
+def _cross_shapes(d):
+    """(shape, strides) of q, of k and v, of out, and of lse."""
+    w, kw = d.heads * d.head_dim, d.kv_heads * d.head_dim
+    qs, ks, os = d.q_stride or w, d.kv_stride or kw, d.out_stride or w
+    return (((d.batch, d.q_len, w), (d.q_len * qs, qs, 1)), ((d.batch, d.kv_len, kw), (d.kv_len * ks, ks, 1)),
+            ((d.batch, d.q_len, w), (d.q_len * os, os, 1)), ((d.batch, d.heads, d.q_len), (d.heads * d.q_len, d.q_len, 1)))
+
+
+def slapo_cross_attn_fwd(desc, q, k, v, kv_lens, out, lse=None, ws=None, stream=None):
+    """q, out [batch, q_len, heads * head_dim], k, v [batch, kv_len, kv_heads * head_dim], views with the descriptor's strides."""
+    need, _ = slapo_cross_attn_workspace(desc)
+    st, dev = _stream_and_device(stream)
+    dt, f32, (a, b, c, e) = _TORCH[desc.dtype], torch.float32, _cross_shapes(desc)
+    _check(lib().slapo_cross_attn_fwd(C.byref(desc), _arg("q", q, dt, *a, dev), _arg("k", k, dt, *b, dev), _arg("v", v, dt, *b, dev),
+                                      _arg("kv_lens", kv_lens, torch.int32, (desc.batch,), (1,), dev, True), _arg("out", out, dt, *c, dev),
+                                      _arg("lse", lse, f32, *e, dev, True), _room("ws", ws, need, dev), st), "slapo_cross_attn_fwd")
+
+
+def slapo_cross_attn_bwd(desc, q, k, v, kv_lens, out, dout, lse, dq, dk, dv, ws, stream=None):
+    _, need = slapo_cross_attn_workspace(desc)
+    st, dev = _stream_and_device(stream)
+    dt, (a, b, c, e) = _TORCH[desc.dtype], _cross_shapes(desc)
+    _check(lib().slapo_cross_attn_bwd(C.byref(desc), _arg("q", q, dt, *a, dev), _arg("k", k, dt, *b, dev), _arg("v", v, dt, *b, dev),
+                                      _arg("kv_lens", kv_lens, torch.int32, (desc.batch,), (1,), dev, True), _arg("out", out, dt, *c, dev),
+                                      _arg("dout", dout, dt, *c, dev), _arg("lse", lse, torch.float32, *e, dev), _arg("dq", dq, dt, *a, dev),
+                                      _arg("dk", dk, dt, *b, dev), _arg("dv", dv, dt, *b, dev), _room("ws", ws, need, dev), st),
+           "slapo_cross_attn_bwd")
+
+
+def make_rope_axes_desc(rows, heads, head_dim, pairs, base=10000.0, ladder=ROPE_SHARED, dtype=BF16, in_stride=0, out_stride=0) -> RopeAxesDesc:
+    """pairs: how many pairs of a head each axis turns."""
+    if len(pairs) > 4:
+        raise ValueError(f"{len(pairs)} axes: at most 4 are supported")
+    return RopeAxesDesc(rows=rows, heads=heads, head_dim=head_dim, axes=len(pairs), pairs=(C.c_int32 * 4)(*pairs), ladder=ladder, base=base,
+                        dtype=dtype, in_stride=in_stride, out_stride=out_stride)
+
+
+def slapo_rope_axes(desc, positions, x, out, inverse=0, stream=None):
+    """x, out: tensors whose rows (all dimensions but the last, `rows` of them, evenly `in_stride` / `out_stride` apart) hold the heads in
+    front; positions int32 [rows, axes]."""
+    st, dev = _stream_and_device(stream)
+    dt, width = _TORCH[desc.dtype], desc.heads * desc.head_dim
+    _check(lib().slapo_rope_axes(C.byref(desc), _arg("positions", positions, torch.int32, (desc.rows, desc.axes), (desc.axes, 1), dev),
+                                 _rows("x", x, dt, desc.rows, width, desc.in_stride or width, dev),
+                                 _rows("out", out, dt, desc.rows, width, desc.out_stride or width, dev), inverse, st), "slapo_rope_axes")
+
+
+def _rows(name, t, dtype, rows, width, stride, device):
+    """Address of a tensor of `rows` rows of at least `width` elements, `stride` apart."""
+    shape, strides = t.shape, t.stride()
+    ok = t.dtype is dtype and t.is_cuda and t.device.index == device and len(shape) >= 1 and shape[-1] >= width and strides[-1] == 1
+    n = 1
+    for size, step in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        ok = ok and (size == 1 or step == n * stride)
+        n *= size
+    if not ok or n != rows:
+        _refuse(name, t, f"{dtype}, {rows} rows of {width} or more elements, {stride} from one to the next,")
+    return t.data_ptr()
+
+
+class GradPlan:
+    """Which gradients take part in a norm, and where the clipped ones go (`out`, tensors of the same types and sizes; None: back where they came
+    from). Built once for arrays that stay where they are; it keeps the tensors alive. One call at a time uses it."""
+
+    def __init__(self, grads, out=None, stream=None):
+        grads = list(grads)
+        out = [None] * len(grads) if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
+        st, self.device = _stream_and_device(stream)
+        table = (_Grad * max(1, len(grads)))()
+        for i, (g, o) in enumerate(zip(grads, out)):
+            for t in (g, o):
+                if t is not None and (t.dtype not in _DTYPE or t.dtype is not g.dtype or t.numel() != g.numel() or not t.is_contiguous()
+                                      or not t.is_cuda or t.device.index != self.device):
+                    _refuse(f"gradient {i}", t, f"contiguous {g.dtype} of {g.numel()} elements")
+            table[i] = _Grad(g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), _DTYPE[g.dtype])
+        need = C.c_size_t(0)
+        _check(lib().slapo_grad_plan_bytes(len(grads), table, C.byref(need)), "slapo_grad_plan_bytes")
+        self.memory = torch.empty(need.value, dtype=torch.uint8, device=f"cuda:{self.device}")
+        self.tensors, self.plan = (grads, out), _GradPlan()
+        _check(lib().slapo_grad_plan_build(len(grads), table, self.memory.data_ptr(), C.byref(self.plan), st), "slapo_grad_plan_build")
+
+
+def _scalar(name, t, dtype, device, optional=False):
+    if t is None and optional:
+        return None
+    if t.dtype is not dtype or t.numel() != 1 or not t.is_cuda or t.device.index != device:
+        _refuse(name, t, f"one {dtype}")
+    return t.data_ptr()
+
+
+def slapo_grad_sumsq(plan: GradPlan, sumsq, accumulate=0, stream=None):
+    """sumsq: one float64."""
+    st, dev = _stream_and_device(stream)
+    if dev != plan.device:
+        raise ValueError(f"the plan belongs to device {plan.device}, the stream to {dev}")
+    _check(lib().slapo_grad_sumsq(C.byref(plan.plan), accumulate, _scalar("sumsq", sumsq, torch.float64, dev), st), "slapo_grad_sumsq")
+
+
+def slapo_grad_clip(plan: GradPlan, sumsq, max_norm, norm=None, stream=None):
+    """norm: one float32, or None."""
+    st, dev = _stream_and_device(stream)
+    if dev != plan.device:
+        raise ValueError(f"the plan belongs to device {plan.device}, the stream to {dev}")
+    _check(lib().slapo_grad_clip(C.byref(plan.plan), _scalar("sumsq", sumsq, torch.float64, dev), max_norm,
+                                 _scalar("norm", norm, torch.float32, dev, True), st), "slapo_grad_clip")
+
+
+def clip_gradients(grads, max_norm):
+    """Clips the gradients in place to a norm of at most max_norm, all of them taken together; returns the norm that they had (one float32 on
+    the device; nothing waits for it). Programs that clip the same arrays step by step keep a GradPlan instead."""
+    plan = GradPlan(grads)
+    sumsq = torch.empty(1, dtype=torch.float64, device=plan.memory.device)
+    norm = torch.empty(1, dtype=torch.float32, device=plan.memory.device)
+    slapo_grad_sumsq(plan, sumsq)
+    slapo_grad_clip(plan, sumsq, max_norm, norm)
+    return norm
+
+
 def slapo_stack_workspace(desc: LayerDesc, n_layers: int):
     a, b, c = C.c_size_t(0), C.c_size_t(0), C.c_size_t(0)
     _check(lib().slapo_stack_workspace(C.byref(desc), n_layers, C.byref(a), C.byref(b), C.byref(c)),
@@ -318,6 +521,10 @@ class Stack:
         slapo_stack_bwd(self.desc, self.params, x, seqlens, dy, self.acts, self.saved, dx, self.grads, self.scratch)
         return dx
 
+    def clip_gradients(self, max_norm):
+        """Of all layers together, in place; returns their norm before."""
+        return clip_gradients([g for layer in self.grads for g in layer.values()], max_norm)
+
 
 class Layer:
     """Convenience holder: device parameters, gradients and the two workspaces of one layer."""
@@ -344,6 +551,10 @@ class Layer:
         dx = torch.empty_like(x)
         slapo_layer_bwd(self.desc, self.params, x, seqlens, dy, self.saved, dx, self.grads, self.scratch)
         return dx
+
+    def clip_gradients(self, max_norm):
+        """In place; returns their norm before."""
+        return clip_gradients(self.grads.values(), max_norm)
 
     def saved_tensor(self, name):
         off, nbytes = slapo_layer_saved_region(self.desc, name)

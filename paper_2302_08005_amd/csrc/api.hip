@@ -5,19 +5,12 @@
 
 #include <mutex>
 
-#include "../../include/slapo.h"
+#include "entry.h"
 #include "kernels.h"
 
 using namespace slapo;
 
 namespace {
-
-inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
-inline bool overlap(const void* a, const void* b, size_t bytes) {   // arrays of `bytes` each
-  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return p < q + bytes && q < p + bytes;
-}
-inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 // width of each of Q, K, V (heads * head dim): the hidden size unless the descriptor says otherwise
 inline int attn_width(const slapo_layer_desc* d) { return d->attn_dim > 0 ? d->attn_dim : d->hidden; }
@@ -112,17 +105,6 @@ AttnShape make_attn_shape(const slapo_layer_desc* d) {
   as.drop.thr = (uint32_t)llround((double)d->attn_dropout_p * 65536.0);
   as.drop.scale = 1.0f / (1.0f - d->attn_dropout_p);
   return as;
-}
-
-// A launch that failed leaves its error in the runtime's per-thread "last error". Every entry point samples that
-// slot before its first launch (entry_error) and again after its last one (finish): an error that was already
-// there belongs to somebody else and is neither reported as ours nor cleared; one that appeared in between is
-// ours, is reported as SLAPO_ERR_HIP and cleared.
-thread_local hipError_t g_error_at_entry = hipSuccess;
-void entry_error() { g_error_at_entry = hipPeekAtLastError(); }
-int finish() {
-  if (g_error_at_entry != hipSuccess) return SLAPO_OK;   // cannot tell ours from the stale one: leave it to its owner
-  return hipGetLastError() == hipSuccess ? SLAPO_OK : SLAPO_ERR_HIP;
 }
 
 // The weight-gradient GEMMs of the backward pass do not feed the data-gradient chain, and most kernels of

@@ -137,4 +137,50 @@ void launch_colreduce3(int dtype, int64_t nblk, int H, const float* partials, vo
                        int accumulate, hipStream_t st);
 void launch_dropout_mask(int64_t n_elements, uint8_t* mask, const DropoutParams& dp, hipStream_t st);
 
+// Cross attention: q_len query tokens of a sample read kv_len states. The query heads that share a key head lie side by side in a
+// token's row, so a key head has q_len * group rows of queries: row r is token r / group, head r % group of the group (CrossRows).
+struct CrossShape {
+  int batch, q_len, kv_len, heads, kv_heads, group;   // group = heads / kv_heads
+  float scale;
+  int64_t q_stride, kv_stride, out_stride;            // elements from one token to the next: q, dq; k, v, dk, dv; out, dout
+  uint32_t div_mul, div_shift;                        // r / group = (high word of r * div_mul, + r) >> div_shift, for r < 2^31
+};
+struct CrossOperands {
+  const void *q, *k, *v;
+  const int32_t* lens;   // visible keys of each sample (NULL: kv_len)
+  const void *out, *dout;
+  void *o, *dq, *dk, *dv;
+  float *lse, *ws;
+};
+size_t cross_attn_fwd_ws_bytes(int dtype, int head_dim, const CrossShape& s);
+size_t cross_attn_bwd_ws_bytes(int dtype, int head_dim, const CrossShape& s);
+void launch_cross_attn_fwd(int dtype, int head_dim, const CrossShape& s, const CrossOperands& p, hipStream_t st);
+void launch_cross_attn_bwd(int dtype, int head_dim, const CrossShape& s, const CrossOperands& p, hipStream_t st);
+
+// Rotary positions of several axes (rope_axes.hip).
+constexpr int ROPE_MAX_AXES = 4, ROPE_MAX_PAIRS = 128;
+struct RopeAxes {
+  int64_t rows, in_stride, out_stride;
+  int heads, head_dim, axes, turned;    // turned: pairs of a head that some axis turns, the first ones
+  int first[ROPE_MAX_AXES + 1];         // axis a turns pairs first[a] .. first[a + 1] - 1
+  int own_ladders, inverse;
+  double log2_base;
+};
+void launch_rope_axes(int dtype, const RopeAxes& r, const int32_t* positions, const void* in, void* out, hipStream_t st);
+
+// Sums of squares and scaling over many arrays (grad_norm.hip). An array is cut into segments of `segment` bytes; the plan's device
+// memory holds a counter, an entry per array, the array of each segment, and a partial sum per block.
+struct GradEntry {
+  const void* in;
+  void* out;
+  int64_t count;
+  int32_t dtype, first;   // first: its first segment
+};
+constexpr int GRAD_BLOCKS = 2048;
+struct GradPlanLayout { size_t entries, map, partials, total; };
+GradPlanLayout grad_plan_layout(int64_t n, int64_t segments);
+void launch_grad_plan(int n, const GradEntry* entries, int64_t segments, int64_t segment, void* memory, hipStream_t st);
+void launch_grad_sumsq(int64_t n, int64_t segments, int64_t segment, void* memory, int accumulate, double* sumsq, hipStream_t st);
+void launch_grad_clip(int64_t n, int64_t segments, int64_t segment, void* memory, const double* sumsq, float max_norm, float* norm, hipStream_t st);
+
 }  // namespace slapo

@@ -1,0 +1,211 @@
+"""Cross attention, forward and backward, against the fp64 definition, element by element within derived bounds."""
+import numpy as np
+import pytest
+import torch
+
+import workloads as W
+from gpu_util import DEV, store, tdtype, to_np
+from oracle import operators as O
+from paper_2302_08005_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+ROUND = {W.FP32: 2.0 ** -24, W.FP16: 2.0 ** -11, W.BF16: 2.0 ** -8}   # half a step, relative
+TINY = {W.FP32: 0.0, W.FP16: 2.0 ** -25, W.BF16: 0.0}                  # half a step among the subnormal numbers of IEEE half
+
+
+def view(a, dtype, stride, gap=np.nan):
+    """[B,S,w] host array -> device view with `stride` elements from token to token, `gap` between the rows; and the array behind it."""
+    b, s, w = a.shape
+    back = torch.full((b, s, stride), gap, dtype=tdtype(dtype), device=DEV)
+    back[..., :w] = torch.from_numpy(np.ascontiguousarray(a)).to(DEV).to(tdtype(dtype))
+    return back[..., :w], back
+
+
+class Problem:
+    def __init__(self, batch, q_len, kv_len, heads, kv_heads, width, dtype=W.BF16, lens=None, scale=0.0, strided=False, big=1.0, seed=0, poison=True):
+        rng = np.random.default_rng(seed + q_len * 1000 + kv_len)
+        self.__dict__.update(batch=batch, q_len=q_len, kv_len=kv_len, heads=heads, kv_heads=kv_heads, width=width, dtype=dtype)
+        w, kw = heads * width, kv_heads * width
+        self.lens = None if lens is None else np.resize(np.array(lens, dtype=np.int32), batch)
+        qs, os_ = (w + 24, w + 8) if strided else (0, 0)
+        ks = 2 * kw if strided else 0   # keys and values side by side
+        self.desc = B.make_cross_attn_desc(batch=batch, q_len=q_len, kv_len=kv_len, heads=heads, kv_heads=kv_heads, head_dim=width, dtype=dtype,
+                                           scale=scale, q_stride=qs, kv_stride=ks, out_stride=os_)
+        self.scale = scale or None
+        q, k, v, do = (store(rng.standard_normal(s), dtype) for s in ((batch, q_len, w), (batch, kv_len, kw), (batch, kv_len, kw), (batch, q_len, w)))
+        q = store(q * big, dtype)
+        if self.lens is not None and poison:   # what lies behind the visible states reaches nothing
+            for b, n in enumerate(np.clip(self.lens, 0, kv_len)):
+                k[b, n:], v[b, n:] = (np.nan, np.inf) if b % 2 else (-np.inf, np.nan)
+        self.host = [x.reshape(*x.shape[:2], -1, width).astype(np.float64) for x in (q, k, v, do)]
+        self.q, self.q_back = view(q, dtype, qs or w)
+        self.do, _ = view(do, dtype, os_ or w)
+        self.out, self.out_back = view(np.zeros_like(do), dtype, os_ or w, gap=7.0)
+        self.dq, self.dq_back = view(np.zeros_like(q), dtype, qs or w, gap=7.0)
+        self.kv, self.dkv = (torch.full((batch, kv_len, 2 * kw), 7.0, dtype=tdtype(dtype), device=DEV) for _ in range(2))
+        if strided:
+            self.kv[..., :kw], self.kv[..., kw:] = (torch.from_numpy(x).to(DEV) for x in (k, v))
+            self.k, self.v, self.dk, self.dv = self.kv[..., :kw], self.kv[..., kw:], self.dkv[..., :kw], self.dkv[..., kw:]
+        else:
+            self.k, self.v = (view(x, dtype, kw)[0] for x in (k, v))
+            self.dk, self.dv = (torch.full((batch, kv_len, kw), 7.0, dtype=tdtype(dtype), device=DEV) for _ in range(2))
+        self.lse = torch.full((batch, heads, q_len), 7.0, device=DEV)
+        self.dlens = None if lens is None else torch.from_numpy(self.lens).to(DEV)
+        need = B.slapo_cross_attn_workspace(self.desc)
+        self.ws = [torch.full((n,), 0xff, dtype=torch.uint8, device=DEV) if n else None for n in need]   # (NaN all over)
+
+    def forward(self, lse=True):
+        B.slapo_cross_attn_fwd(self.desc, self.q, self.k, self.v, self.dlens, self.out, self.lse if lse else None, self.ws[0])
+
+    def backward(self):
+        B.slapo_cross_attn_bwd(self.desc, self.q, self.k, self.v, self.dlens, self.out, self.do, self.lse, self.dq, self.dk, self.dv, self.ws[1])
+
+    def heads_of(self, t):
+        return to_np(t).reshape(*t.shape[:2], -1, self.width)
+
+    def check(self, backward=True):
+        q, k, v, do = self.host
+        self.forward()
+        out, lse = O.cross_forward(q, k, v, self.lens, self.scale)
+        stored = self.heads_of(self.out)
+        bounds = O.cross_bounds(q, k, v, do, self.lens, self.scale, stored, ROUND[self.dtype], TINY[self.dtype])
+        within(stored, out, bounds[0], "out")
+        got = to_np(self.lse)
+        assert np.array_equal(np.isneginf(got), np.isneginf(lse))
+        seen = np.isfinite(lse)
+        within(got[seen], lse[seen], bounds[1][seen], "lse")
+        if backward:
+            self.backward()
+            for name, want, bound in zip(("dq", "dk", "dv"), O.cross_backward(q, k, v, do, self.lens, self.scale, stored), bounds[2:]):
+                within(self.heads_of(getattr(self, name)), want, bound, name)
+        for back, w in ((self.out_back, self.out), (self.dq_back, self.dq)):   # columns between the rows are left alone
+            gap = back[..., w.shape[-1]:]
+            assert gap.numel() == 0 or bool((gap == 7.0).all())
+
+
+def within(got, want, bound, name):
+    off = np.abs(got - want)
+    ok = off <= bound   # (NaN: not)
+    assert ok.all(), (name, int((~ok).sum()), ok.size, np.argwhere(~ok)[:3].tolist(), float(np.nanmax(off / bound)))
+
+
+SHAPES = [   # batch, q_len, kv_len, heads, kv_heads, head width
+    (1, 1, 1, 1, 1, 64), (2, 1, 70, 4, 4, 64), (3, 1, 1000, 8, 2, 128), (2, 5, 33, 6, 2, 64), (1, 129, 257, 2, 1, 128), (3, 64, 64, 4, 4, 64),
+    (2, 200, 77, 8, 2, 128), (1, 31, 1000, 2, 2, 64), (2, 333, 130, 6, 2, 64), (1, 1, 5000, 3, 1, 64), (1, 700, 1, 2, 2, 128), (9, 3, 15, 5, 5, 128),
+    (1, 65, 2100, 12, 1, 64), (2, 1100, 300, 2, 2, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_all_states_visible(shape, dtype):
+    Problem(*shape, dtype=dtype, big=2.0).check()
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s[2] > 1], ids=lambda s: "x".join(map(str, s)))
+def test_lengths_with_infinities_and_nan_behind_them_and_strides(shape, dtype):
+    kv = shape[2]
+    lens = [kv // 2 + 1, 0, kv, 1, kv + 5, -4, kv - 1, min(kv, 64), min(kv, 65)]
+    start = shape[1] % 3
+    Problem(*shape, dtype=dtype, lens=lens[start:] + lens[:start], strided=True).check()
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
+def test_every_length_around_a_tile(dtype):
+    Problem(70, 3, 69, 2, 1, 64, dtype=dtype, lens=list(range(70))).check()
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("scale", [0.01, 1.0])
+def test_scales(dtype, scale):
+    Problem(2, 70, 150, 4, 2, 64, dtype=dtype, scale=scale, lens=[150, 99]).check()
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP32], ids=["bf16", "fp32"])
+def test_a_state_that_takes_a_row_alone(dtype):
+    """Scores of up to several hundred: the softmax is one state, late in the walk, and every earlier sum is scaled away."""
+    p = Problem(1, 40, 700, 2, 2, 64, dtype=dtype, big=1.0, lens=[650])
+    q, k = p.host[0], p.host[1]
+    k[0, 640] = store(q[0, 7] * 16, dtype)
+    p.k[0, 640] = torch.from_numpy(k[0, 640].reshape(-1)).to(DEV)
+    p.check()
+
+
+def test_without_lse_and_the_same_bits_again():
+    p = Problem(3, 20, 500, 4, 2, 64, lens=[500, 0, 321])
+    p.forward()
+    p.backward()
+    first = [x.clone() for x in (p.out, p.lse, p.dq, p.dk, p.dv)]
+    p.out.zero_()
+    p.forward(lse=False)
+    assert torch.equal(p.out, first[0])
+    p.forward()
+    p.backward()
+    for a, b in zip(first, (p.out, p.lse, p.dq, p.dk, p.dv)):
+        assert torch.equal(a, b)
+
+
+def test_gradients_against_differences():
+    """Of sum(out * dout) in the fp32 mode: central differences along random directions, fp64 sums of fp32 outputs (2^-24 of a sum of
+    ~5e3 terms of size 1 over a step of 2^-4: 3e-4 off at most by rounding; the third-order term is below 1e-3 of the slope's scale)."""
+    p = Problem(2, 9, 40, 4, 2, 64, dtype=W.FP32, lens=[40, 23], poison=False)
+    p.forward()
+    p.backward()
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for t, g in ((p.q, p.dq), (p.k, p.dk), (p.v, p.dv)):
+        way = torch.randn(t.shape, device=DEV, generator=gen)
+        way /= way.norm()
+        old, f = t.clone(), []
+        for h in (2.0 ** -4, -2.0 ** -4):
+            t.copy_(old + h * way)
+            p.forward()
+            f.append((p.out.double() * p.do.double()).sum().item())
+        t.copy_(old)
+        slope, want = (f[0] - f[1]) / 2.0 ** -3, (g.double() * way.double()).sum().item()
+        assert abs(slope - want) <= 3e-4 + 1e-3 * g.double().norm().item(), (slope, want)
+
+
+def test_refused_tensors():
+    """What the library cannot see is refused before an address is taken: other types, extents, strides and places."""
+    p = Problem(2, 5, 33, 4, 2, 64)
+    ok = dict(q=p.q, k=p.k, v=p.v, kv_lens=None, out=p.out, lse=p.lse, ws=p.ws[0])
+    bad = [dict(q=p.q.float()), dict(q=p.q[:, :4]), dict(k=p.k[..., :64]), dict(k=p.k.transpose(0, 1).contiguous().transpose(0, 1)), dict(v=p.v.cpu()),
+           dict(out=p.out.half()), dict(lse=p.lse[:, :3]), dict(kv_lens=torch.ones(2, dtype=torch.int64, device=DEV)),
+           dict(kv_lens=torch.ones(3, dtype=torch.int32, device=DEV))]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            B.slapo_cross_attn_fwd(p.desc, **{**ok, **kw})
+    p.forward()
+    with pytest.raises(ValueError):
+        B.slapo_cross_attn_bwd(p.desc, p.q, p.k, p.v, None, p.out, p.do, p.lse, p.dq, p.dk, p.dv, p.ws[1][:-4])
+    with pytest.raises(ValueError):
+        B.slapo_cross_attn_bwd(p.desc, p.q, p.k, p.v, None, p.out, p.do, p.lse, p.dq, p.dk, p.dv, None)
+
+
+def test_on_another_stream_and_replayed():
+    """Captured forward and backward, replayed on new inputs between eager calls, against the eager results."""
+    p = Problem(2, 37, 600, 4, 2, 64, lens=[600, 401])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        p.forward()
+        p.backward()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.forward()
+        p.backward()
+    for i in range(4):
+        p.q.copy_(torch.randn(p.q.shape, device=DEV))
+        p.dlens.copy_(torch.tensor([600 - 100 * i, 64 * i], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (p.out, p.lse, p.dq, p.dk, p.dv)]
+        for x in (p.out, p.lse, p.dq, p.dk, p.dv):
+            x.fill_(3.0)
+        p.forward()
+        p.backward()
+        for a, b in zip(got, (p.out, p.lse, p.dq, p.dk, p.dv)):
+            assert torch.equal(a, b), i

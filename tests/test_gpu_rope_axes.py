@@ -1,0 +1,104 @@
+"""Rotary positions of several axes against the fp64 definition, element by element within derived bounds."""
+import numpy as np
+import pytest
+import torch
+
+import workloads as W
+from gpu_util import DEV, store, tdtype, to_np
+from oracle import operators as O
+from paper_2302_08005_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+ROUND = {W.FP32: 2.0 ** -24, W.FP16: 2.0 ** -11, W.BF16: 2.0 ** -8}
+TINY = {W.FP32: 2.0 ** -150, W.FP16: 2.0 ** -25, W.BF16: 2.0 ** -134}   # half a step among the subnormal numbers
+DTYPES = pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
+
+
+def problem(rows, heads, width, axes, dtype, extra_in, far, seed=0):
+    rng = np.random.default_rng(seed + rows * 100 + heads)
+    x = store(rng.standard_normal((rows, heads * width)), dtype)
+    pos = rng.integers(-far, far, (rows, axes)).astype(np.int32)
+    dx = torch.full((rows, heads * width + extra_in), float("nan"), dtype=tdtype(dtype), device=DEV)
+    dx[:, :heads * width] = torch.from_numpy(x).to(DEV)
+    return x.reshape(rows, heads, width).astype(np.float64), pos, dx, torch.from_numpy(pos).to(DEV)
+
+
+CASES = [   # rows, heads, head width, pairs of each axis, per axis, base
+    (1, 1, 8, (4,), False, 10000.0), (1, 40, 128, (16, 24, 24), False, 10000.0), (577, 16, 64, (16, 16), True, 10000.0),
+    (300, 3, 72, (12, 12, 12), True, 100.0), (65, 5, 80, (7, 0, 11, 3), False, 500000.0), (33, 2, 256, (128,), False, 1.5), (4100, 2, 16, (3, 2), True, 10000.0),
+    (17, 300, 8, (1, 1), False, 10000.0), (5, 1, 64, (0, 0), True, 10.0),
+]
+
+
+@DTYPES
+@pytest.mark.parametrize("inverse", [0, 1])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}")
+def test_against_the_definition(case, inverse, dtype):
+    rows, heads, width, pairs, per_axis, base = case
+    x, pos, dx, dpos = problem(rows, heads, width, len(pairs), dtype, 24, 3000)
+    y = torch.full((rows, heads * width + 8), 5.0, dtype=tdtype(dtype), device=DEV)
+    d = B.make_rope_axes_desc(rows, heads, width, pairs, base, B.ROPE_PER_AXIS if per_axis else B.ROPE_SHARED, dtype, dx.stride(0), y.stride(0))
+    before = dx.clone()
+    B.slapo_rope_axes(d, dpos, dx, y, inverse)
+    want = O.rotary(x, pos, pairs, base, per_axis, bool(inverse))
+    got = to_np(y[:, :heads * width]).reshape(want.shape)
+    assert (np.abs(got - want) <= O.rotary_bound(x, want, pos, pairs, ROUND[dtype], TINY[dtype], base, per_axis)).all()
+    t = 2 * sum(pairs)
+    assert np.array_equal(got[..., t:], x[..., t:])                                # pairs of no axis
+    assert bool((y[:, heads * width:] == 5.0).all())                               # columns behind the heads
+    assert torch.equal(dx[:, :heads * width], before[:, :heads * width])
+    # in place: the same bits, and what lies behind the heads stays (NaN)
+    d2 = B.make_rope_axes_desc(rows, heads, width, pairs, base, B.ROPE_PER_AXIS if per_axis else B.ROPE_SHARED, dtype, dx.stride(0), dx.stride(0))
+    B.slapo_rope_axes(d2, dpos, dx, dx, inverse)
+    assert torch.equal(dx[:, :heads * width], y[:, :heads * width]) and bool(dx[:, heads * width:].isnan().all())
+
+
+def test_far_positions():
+    """Up to the ends of 32 bits, either sign."""
+    x, pos, dx, dpos = problem(200, 2, 64, 2, W.FP32, 0, 2 ** 31 - 1)
+    y = torch.empty_like(dx)
+    B.slapo_rope_axes(B.make_rope_axes_desc(200, 2, 64, (16, 16), dtype=W.FP32), dpos, dx, y)
+    want = O.rotary(x, pos, (16, 16))
+    bound = O.rotary_bound(x, want, pos, (16, 16), ROUND[W.FP32], TINY[W.FP32])
+    assert (np.abs(to_np(y).reshape(want.shape) - want) <= bound).all() and bound.max() < 2e-5
+
+
+def test_infinities_in_pairs_of_no_axis_stay():
+    x = torch.full((3, 64), float("inf"), device=DEV)
+    y = torch.empty_like(x)
+    pos = torch.arange(3, dtype=torch.int32, device=DEV)[:, None]
+    x[:, :8] = 1.0
+    B.slapo_rope_axes(B.make_rope_axes_desc(3, 1, 64, (4,), dtype=W.FP32), pos, x, y)
+    assert bool(y[:, :8].isfinite().all()) and bool((y[:, 8:] == float("inf")).all())
+
+
+@DTYPES
+def test_one_axis_is_the_layers_rotary(dtype):
+    """Queries and keys of a packed projection, positions from 0 in every sequence: slapo_rope, but for the last bits of its 32-bit table."""
+    batch, seq, heads, width = 3, 50, 4, 64
+    desc = B.make_desc(batch=batch, seq=seq, hidden=heads * width, heads=heads, ffn=64, arch=B.LLAMA, pre_ln=1, dtype=dtype)
+    rng = np.random.default_rng(1)
+    qkv = torch.from_numpy(store(rng.standard_normal((batch, seq, 3 * heads * width)), dtype)).to(DEV).to(tdtype(dtype))
+    mine = qkv.clone()
+    B.slapo_rope(desc, qkv, torch.empty(seq * width // 2 * 2, device=DEV))
+    pos = torch.arange(seq, dtype=torch.int32, device=DEV).repeat(batch)[:, None]
+    d = B.make_rope_axes_desc(batch * seq, 2 * heads, width, (width // 2,), dtype=dtype, in_stride=3 * heads * width, out_stride=3 * heads * width)
+    B.slapo_rope_axes(d, pos, mine, mine)
+    # (each is within u of the value and 1e-6 of the pair's length)
+    assert bool(((mine.double() - qkv.double()).abs() <= 2 * ROUND[dtype] * qkv.double().abs() * 1.01 + 2e-5).all())
+    assert torch.equal(mine[..., 2 * heads * width:], qkv[..., 2 * heads * width:])
+
+
+def test_refused_tensors():
+    x, pos, dx, dpos = problem(6, 2, 64, 2, W.BF16, 8, 100)
+    y = torch.empty((6, 128), dtype=torch.bfloat16, device=DEV)
+    d = B.make_rope_axes_desc(6, 2, 64, (16, 16), in_stride=136)
+    for p, a, b in ((dpos.long(), dx, y), (dpos[:, :1], dx, y), (dpos[:5], dx, y), (dpos, dx[:5], y), (dpos, dx.float(), y), (dpos, dx.cpu(), y),
+                    (dpos, y, y), (dpos, dx, dx), (dpos, dx, y[:, :120])):
+        with pytest.raises(ValueError):
+            B.slapo_rope_axes(d, p, a, b)
+    flat = torch.zeros(6 * 136 + 8, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(B.SlapoError) as e:   # in and out share memory without being the same rows
+        B.slapo_rope_axes(B.make_rope_axes_desc(6, 2, 64, (16, 16), in_stride=136, out_stride=136), dpos, flat[:6 * 136].view(6, 136), flat[8:].view(6, 136))
+    assert e.value.status == -2
