@@ -33,13 +33,12 @@ def cross_forward(q, k, v, lens=None, scale=None):
     return (p @ v).transpose(0, 2, 1, 3), lse
 
 
-def cross_backward(q, k, v, dout, lens=None, scale=None, out=None):
-    """dq, dk, dv in the shapes of q, k, v. out: the forward's output where delta = dout . out is to be taken of a stored one."""
+def cross_backward(q, k, v, dout, lens=None, scale=None):
+    """dq, dk, dv in the shapes of q, k, v."""
     scale = q.shape[-1] ** -0.5 if scale is None else scale
     group = q.shape[2] // k.shape[2]
     s, kk, vv = _scores(q, k, v, lens, scale)
     o, lse = cross_forward(q, k, v, lens, scale)
-    o = o if out is None else out
     with np.errstate(invalid="ignore"):
         p = np.where(np.isfinite(s), np.exp(s - lse[..., None]), 0.0)
     do, qt = dout.transpose(0, 2, 1, 3), q.transpose(0, 2, 1, 3)
@@ -52,8 +51,9 @@ def cross_backward(q, k, v, dout, lens=None, scale=None, out=None):
             over_group(p.transpose(0, 1, 3, 2) @ do))
 
 
-def cross_bounds(q, k, v, dout, lens, scale, out, u, tiny):
-    """Bounds on the errors of (out, lse, dq, dk, dv), given `out` as backward reads it.
+def cross_bounds(q, k, v, dout, lens, scale, u, tiny, stored_above):
+    """Bounds on the errors of (out, lse, dq, dk, dv). In samples of more than `stored_above` visible states backward takes delta = dout . out of the
+    stored out, which is off by its own bound, else as the sum of p dp.
 
     e = 2^-24. A score is a sum of d products: off by at most (d + 2) e scale sum|q k|, and with the exponential (3e relative, and the
     argument's own rounding, 2e times its size) a probability by `es` relative; its row sum as much again, and n e for the additions. What
@@ -75,8 +75,12 @@ def cross_bounds(q, k, v, dout, lens, scale, out, u, tiny):
     b_lse = (row + 2 * e * (1 + size))[..., 0]
     ep = es + row + 2 * e * (1 + size)           # of a probability taken from lse, relative
     dp = do @ vv.transpose(0, 1, 3, 2)
-    delta = (do * out.transpose(0, 2, 1, 3)).sum(-1, keepdims=True)
-    sums = (d + 2) * e * (np.abs(do) @ np.abs(vv).transpose(0, 1, 3, 2) + (np.abs(do) * np.abs(out.transpose(0, 2, 1, 3))).sum(-1, keepdims=True))
+    delta = (do * o.transpose(0, 2, 1, 3)).sum(-1, keepdims=True)
+    seen = np.isfinite(s).any(2, keepdims=True).sum(-1, keepdims=True)
+    size_dp = np.abs(do) @ np.abs(vv).transpose(0, 1, 3, 2)   # (as much for delta = sum p dp, and n e and es more for its sum)
+    size_delta = (p * size_dp).sum(-1, keepdims=True)
+    sums = (d + 2) * e * (size_dp + size_delta) + (es + row + (n + 4) * e) * size_delta + \
+        np.where(seen > stored_above, (np.abs(do) * (b_out + tiny)).sum(-1, keepdims=True), 0.0)
     ds = p * (dp - delta)
     b_ds = p * sums + np.abs(ds) * (ep + u + 2 * e) + tiny
     b_p = p * (ep + u) + tiny
@@ -86,7 +90,7 @@ def cross_bounds(q, k, v, dout, lens, scale, out, u, tiny):
 
     hidden = np.isinf(s)   # (exactly 0 there)
     b_ds, b_p = np.where(hidden, 0.0, b_ds), np.where(hidden, 0.0, b_p)
-    dq, dk, dv = cross_backward(q, k, v, dout, lens, scale, out)
+    dq, dk, dv = cross_backward(q, k, v, dout, lens, scale)
     b_dq = u * np.abs(dq) + ((b_ds + (n + 4) * e * np.abs(ds)) @ np.abs(kk)).transpose(0, 2, 1, 3) * scale
     b_dk = u * np.abs(dk) + over_group((b_ds + (m + 4) * e * np.abs(ds)).transpose(0, 1, 3, 2) @ np.abs(qt)) * scale
     b_dv = u * np.abs(dv) + over_group((b_p + (m + 4) * e * p).transpose(0, 1, 3, 2) @ np.abs(do))

@@ -6,12 +6,12 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslapo_mi355x.so")
-SOURCES = ("api.hip", "api_operators.hip", "gemm.hip", "grads.hip", "products.hip", "attention.hip", "cross_attention.hip", "rowwise.hip",
-           "rope_axes.hip", "grad_norm.hip")
+SOURCES = ("api.hip", "api_operators.hip", "gemm.hip", "grads.hip", "products.hip", "attention.hip", "cross_attention.hip",
+           "cross_tiles.hip", "rowwise.hip", "rope_axes.hip", "grad_norm.hip")
 # per-file extra flags: the attention kernels alternate MFMA and vector work on the same tiles, so their MFMA
 # results are kept in ordinary VGPRs (the default puts them in accumulation registers and copies them back
 # and forth for every softmax)
-EXTRA = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for name in ("attention.hip", "cross_attention.hip")}
+EXTRA = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for name in ("attention.hip", "cross_tiles.hip")}
 # kernels start on pages of 4 KB: a step launches a different one each time, whose code is fetched anew, and every page that it touches
 # costs. Three decoder layers of 72 tokens, hidden 1088, backward, with kernels on 256 / 1024 / 2048 / 4096 bytes: 185.9 / 185.1 / 184.3 /
 # 182.5 us; an encoder layer of 2 x 824 tokens, hidden 384, checkpointed, 192.8 / 190.9 / 191.1 / 191.0. (5 MB of padding.)

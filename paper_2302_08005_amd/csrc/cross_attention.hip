@@ -1,71 +1,28 @@
 // Cross attention: the query tokens of a sample attend to the states of another sequence (an encoder's, of another length, with a
 // visible length per sample). o_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), s_ij = scale q_i . k_j over the visible j.
 //
-// Query heads that share a key head are one array of rows for it: q_len * group rows, token after token and head after head
-// (CrossRows), so the gradients of a key head add up over its query heads inside a block, in a fixed order.
-//
-// General kernels, for every element type: a block of four wavefronts owns 16 rows (queries, or states for dK/dV) of one (sample, key
+// 16-bit types: cross_tiles.hip. Here the fp32 mode, which checks others: a block of four wavefronts owns 16 rows (queries, or states for dK/dV) of one (sample, key
 // head) and walks the other sequence in chunks of CHUNK. Products on v_mfma_f32_16x16x4_f32: inputs, products and sums in 32 bits. The four
 // wavefronts share the chunk's score tiles of 16 x 16, whose softmax values stay in LDS, then, behind a barrier, the 16-wide column tiles of
 // the outputs. States beyond the visible length are read as zeros, whatever lies there.
 #include <algorithm>
 
-#include "common.h"
-#include "kernels.h"
+#include "cross_attention.h"
 
 namespace slapo {
 
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
-
-// Rows of one (sample, key head): of q, out and their gradients, and of lse and delta.
-struct CrossRows {
-  int group, q_len;
-  uint32_t mul, shift;
-  __device__ __forceinline__ CrossRows(const CrossShape& s) : group(s.group), q_len(s.q_len), mul(s.div_mul), shift(s.div_shift) {}
-  __device__ __forceinline__ int count() const { return q_len * group; }
-  __device__ __forceinline__ int token(int r) const { return (int)((__umulhi((uint32_t)r, mul) + (uint32_t)r) >> shift); }
-  // elements from the sample's first token and the group's first head
-  __device__ __forceinline__ int64_t at(int r, int64_t stride, int width) const {
-    const int t = token(r);
-    return t * stride + (int64_t)(r - t * group) * width;
-  }
-  __device__ __forceinline__ int64_t stat(int r) const {   // in [group][q_len]
-    const int t = token(r);
-    return (int64_t)(r - t * group) * q_len + t;
-  }
-};
-
-__device__ __forceinline__ int visible(const CrossShape& s, const int32_t* lens, int b) {
-  if (!lens) return s.kv_len;
-  const int n = lens[b];
-  return n < 0 ? 0 : n < s.kv_len ? n : s.kv_len;
-}
-
-// ======================================= general kernels =========================================
 constexpr int CHUNK = 128, PITCH = CHUNK + 4;   // floats per LDS row: 16 rows x 16 bytes meet every bank once
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const bf16_t* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return make_float4(bf16lo_to_f32(w.x), bf16hi_to_f32(w.x), bf16lo_to_f32(w.y), bf16hi_to_f32(w.y));
-}
-__device__ __forceinline__ float4 load4(const f16_t* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return make_float4(unpack_lo<true>(w.x), unpack_hi<true>(w.x), unpack_lo<true>(w.y), unpack_hi<true>(w.y));
-}
 __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
-__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) { *reinterpret_cast<uint2*>(p) = make_uint2(pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3])); }
-__device__ __forceinline__ void store4(f16_t* p, const float (&v)[4]) { *reinterpret_cast<uint2*>(p) = make_uint2(pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3])); }
 
 // 16 rows x D, this lane's share: row lane % 16, columns 16 c + 4 (lane / 16) ..; a row that is not there: zeros
 template <int D>
 struct RowFrags {
   float4 v[D / 16];
-  template <typename T>
-  __device__ __forceinline__ void load(const T* row, int g, bool there) {
+  __device__ __forceinline__ void load(const float* row, int g, bool there) {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) v[c] = there ? load4(row + 16 * c + 4 * g) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
@@ -111,8 +68,8 @@ __device__ __forceinline__ float over16(float v, Op&& op) {
 __device__ __forceinline__ float sum2(float a, float b) { return a + b; }
 __device__ __forceinline__ float max2(float a, float b) { return fmaxf(a, b); }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_fwd_general_kernel(CrossShape sh, CrossOperands p) {
+template <int D>
+__global__ __launch_bounds__(256) void cross_fwd_f32_kernel(CrossShape sh, CrossOperands p) {
   __shared__ __attribute__((aligned(16))) float prob[16 * PITCH];
   __shared__ float top[16], total[16], shrink[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
@@ -120,9 +77,9 @@ __global__ __launch_bounds__(256) void cross_fwd_general_kernel(CrossShape sh, C
   const CrossRows rows(sh);
   const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), my_row = min(r0 + i, n_rows - 1);
   const int64_t head0 = (int64_t)h * sh.group * D;
-  const T* q = (const T*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
-  const T* k = (const T*)p.k + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
-  const T* v = (const T*)p.v + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const float* q = (const float*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
+  const float* k = (const float*)p.k + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const float* v = (const float*)p.v + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   RowFrags<D> qf;
   qf.load(q + rows.at(my_row, sh.q_stride, D), g, true);
   constexpr int MINE = D / 64;
@@ -169,15 +126,15 @@ __global__ __launch_bounds__(256) void cross_fwd_general_kernel(CrossShape sh, C
     for (int m = 0; m < MINE; ++m) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[m][r] *= less;
-      const T* col = v + j0 * sh.kv_stride + 16 * (wave + 4 * m) + i;
-      acc[m] = weighted_rows(acc[m], prob + i * PITCH, n, g, [&](int row) { return to_f32(col[row * sh.kv_stride]); });
+      const float* col = v + j0 * sh.kv_stride + 16 * (wave + 4 * m) + i;
+      acc[m] = weighted_rows(acc[m], prob + i * PITCH, n, g, [&](int row) { return col[row * sh.kv_stride]; });
     }
     __syncthreads();
   }
   __syncthreads();
   if (r0 + i < n_rows) {
     const float sum = total[i], inv = sum != 0.f ? 1.f / sum : 0.f;   // (a sum that is no number stays one)
-    T* o = (T*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(r0 + i, sh.out_stride, D);
+    float* o = (float*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(r0 + i, sh.out_stride, D);
 #pragma unroll
     for (int m = 0; m < MINE; ++m) {
       const float out[4] = {acc[m][0] * inv, acc[m][1] * inv, acc[m][2] * inv, acc[m][3] * inv};
@@ -189,8 +146,8 @@ __global__ __launch_bounds__(256) void cross_fwd_general_kernel(CrossShape sh, C
 }
 
 // dQ of 16 rows; also leaves delta = rowsum(dO * O) of its rows in p.ws, laid out as lse, for the other kernel.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_dq_general_kernel(CrossShape sh, CrossOperands p) {
+template <int D>
+__global__ __launch_bounds__(256) void cross_dq_f32_kernel(CrossShape sh, CrossOperands p) {
   __shared__ __attribute__((aligned(16))) float grad[16 * PITCH];
   __shared__ float delta[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
@@ -198,14 +155,14 @@ __global__ __launch_bounds__(256) void cross_dq_general_kernel(CrossShape sh, Cr
   const CrossRows rows(sh);
   const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), my_row = min(r0 + i, n_rows - 1);
   const int64_t head0 = (int64_t)h * sh.group * D, stats = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
-  const T* q = (const T*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
-  const T* k = (const T*)p.k + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
-  const T* v = (const T*)p.v + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const float* q = (const float*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
+  const float* k = (const float*)p.k + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const float* v = (const float*)p.v + (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   const int64_t out0 = (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(my_row, sh.out_stride, D);
   RowFrags<D> qf, df, of;
   qf.load(q + rows.at(my_row, sh.q_stride, D), g, true);
-  df.load((const T*)p.dout + out0, g, true);
-  of.load((const T*)p.out + out0, g, true);
+  df.load((const float*)p.dout + out0, g, true);
+  of.load((const float*)p.out + out0, g, true);
   const float lse = p.lse[stats + rows.stat(my_row)];
   float my_delta = 0.f;
 #pragma unroll
@@ -237,13 +194,13 @@ __global__ __launch_bounds__(256) void cross_dq_general_kernel(CrossShape sh, Cr
     __syncthreads();
 #pragma unroll
     for (int m = 0; m < MINE; ++m) {
-      const T* col = k + j0 * sh.kv_stride + 16 * (wave + 4 * m) + i;
-      acc[m] = weighted_rows(acc[m], grad + i * PITCH, n, g, [&](int row) { return to_f32(col[row * sh.kv_stride]); });
+      const float* col = k + j0 * sh.kv_stride + 16 * (wave + 4 * m) + i;
+      acc[m] = weighted_rows(acc[m], grad + i * PITCH, n, g, [&](int row) { return col[row * sh.kv_stride]; });
     }
     __syncthreads();
   }
   if (r0 + i < n_rows) {
-    T* o = (T*)p.dq + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(r0 + i, sh.q_stride, D);
+    float* o = (float*)p.dq + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(r0 + i, sh.q_stride, D);
 #pragma unroll
     for (int m = 0; m < MINE; ++m) {
       const float out[4] = {acc[m][0] * sh.scale, acc[m][1] * sh.scale, acc[m][2] * sh.scale, acc[m][3] * sh.scale};
@@ -253,21 +210,21 @@ __global__ __launch_bounds__(256) void cross_dq_general_kernel(CrossShape sh, Cr
 }
 
 // dK and dV of 16 states; hidden ones get zeros.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_dkdv_general_kernel(CrossShape sh, CrossOperands p) {
+template <int D>
+__global__ __launch_bounds__(256) void cross_dkdv_f32_kernel(CrossShape sh, CrossOperands p) {
   __shared__ __attribute__((aligned(16))) float prob[16 * PITCH], grad[16 * PITCH];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
   const int b = blockIdx.z, h = blockIdx.y, k0 = blockIdx.x * 16;
   const CrossRows rows(sh);
   const int n_keys = visible(sh, p.lens, b), n_rows = k0 < n_keys ? rows.count() : 0;
   const int64_t head0 = (int64_t)h * sh.group * D, stats = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
-  const T* q = (const T*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
-  const T* dout = (const T*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0;
+  const float* q = (const float*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
+  const float* dout = (const float*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0;
   const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   const bool seen = k0 + i < n_keys;
   RowFrags<D> kf, vf;
-  kf.load((const T*)p.k + kv0 + min(k0 + i, sh.kv_len - 1) * sh.kv_stride, g, seen);
-  vf.load((const T*)p.v + kv0 + min(k0 + i, sh.kv_len - 1) * sh.kv_stride, g, seen);
+  kf.load((const float*)p.k + kv0 + min(k0 + i, sh.kv_len - 1) * sh.kv_stride, g, seen);
+  vf.load((const float*)p.v + kv0 + min(k0 + i, sh.kv_len - 1) * sh.kv_stride, g, seen);
   constexpr int MINE = D / 64;
   f32x4_t dk[MINE], dv[MINE];
 #pragma unroll
@@ -296,8 +253,8 @@ __global__ __launch_bounds__(256) void cross_dkdv_general_kernel(CrossShape sh, 
 #pragma unroll
     for (int m = 0; m < MINE; ++m) {
       const int col = 16 * (wave + 4 * m) + i;
-      dv[m] = weighted_rows(dv[m], prob + i * PITCH, n, g, [&](int row) { return to_f32(dout[rows.at(r0 + row, sh.out_stride, D) + col]); });
-      dk[m] = weighted_rows(dk[m], grad + i * PITCH, n, g, [&](int row) { return to_f32(q[rows.at(r0 + row, sh.q_stride, D) + col]); });
+      dv[m] = weighted_rows(dv[m], prob + i * PITCH, n, g, [&](int row) { return dout[rows.at(r0 + row, sh.out_stride, D) + col]; });
+      dk[m] = weighted_rows(dk[m], grad + i * PITCH, n, g, [&](int row) { return q[rows.at(r0 + row, sh.q_stride, D) + col]; });
     }
     __syncthreads();
   }
@@ -308,38 +265,37 @@ __global__ __launch_bounds__(256) void cross_dkdv_general_kernel(CrossShape sh, 
       const int col = 16 * (wave + 4 * m) + 4 * g;
       const float a[4] = {dk[m][0] * sh.scale, dk[m][1] * sh.scale, dk[m][2] * sh.scale, dk[m][3] * sh.scale};
       const float c[4] = {dv[m][0], dv[m][1], dv[m][2], dv[m][3]};
-      store4((T*)p.dk + at + col, a);
-      store4((T*)p.dv + at + col, c);
+      store4((float*)p.dk + at + col, a);
+      store4((float*)p.dv + at + col, c);
     }
   }
 }
 
-template <typename T, int D>
-void fwd_general(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
+template <int D>
+void fwd_f32(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   const unsigned blocks = (unsigned)(((int64_t)s.q_len * s.group + 15) / 16);
-  hipLaunchKernelGGL((cross_fwd_general_kernel<T, D>), dim3(blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
+  hipLaunchKernelGGL((cross_fwd_f32_kernel<D>), dim3(blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
 }
-template <typename T, int D>
-void bwd_general(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
+template <int D>
+void bwd_f32(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   const unsigned blocks = (unsigned)(((int64_t)s.q_len * s.group + 15) / 16);
-  hipLaunchKernelGGL((cross_dq_general_kernel<T, D>), dim3(blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
-  hipLaunchKernelGGL((cross_dkdv_general_kernel<T, D>), dim3((s.kv_len + 15) / 16, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
+  hipLaunchKernelGGL((cross_dq_f32_kernel<D>), dim3(blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
+  hipLaunchKernelGGL((cross_dkdv_f32_kernel<D>), dim3((s.kv_len + 15) / 16, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
 }
 
 }  // namespace
 
-size_t cross_attn_fwd_ws_bytes(int, int, const CrossShape&) { return 0; }
-size_t cross_attn_bwd_ws_bytes(int, int, const CrossShape& s) { return (size_t)s.batch * s.heads * s.q_len * sizeof(float); }
-
+size_t cross_attn_fwd_ws_bytes(int dtype, int head_dim, const CrossShape& s) { return dtype == DT_FP32 ? 0 : cross_tiles_fwd_ws_bytes(head_dim, s); }
+size_t cross_attn_bwd_ws_bytes(int dtype, int head_dim, const CrossShape& s) {
+  return dtype == DT_FP32 ? (size_t)s.batch * s.heads * s.q_len * sizeof(float) : cross_tiles_bwd_ws_bytes(head_dim, s);
+}
 void launch_cross_attn_fwd(int dtype, int head_dim, const CrossShape& s, const CrossOperands& p, hipStream_t st) {
-  if (dtype == DT_FP32) head_dim == 64 ? fwd_general<float, 64>(s, p, st) : fwd_general<float, 128>(s, p, st);
-  else if (dtype == DT_FP16) head_dim == 64 ? fwd_general<f16_t, 64>(s, p, st) : fwd_general<f16_t, 128>(s, p, st);
-  else head_dim == 64 ? fwd_general<bf16_t, 64>(s, p, st) : fwd_general<bf16_t, 128>(s, p, st);
+  if (dtype != DT_FP32) launch_cross_tiles_fwd(dtype == DT_FP16, head_dim, s, p, st);
+  else head_dim == 64 ? fwd_f32<64>(s, p, st) : fwd_f32<128>(s, p, st);
 }
 void launch_cross_attn_bwd(int dtype, int head_dim, const CrossShape& s, const CrossOperands& p, hipStream_t st) {
-  if (dtype == DT_FP32) head_dim == 64 ? bwd_general<float, 64>(s, p, st) : bwd_general<float, 128>(s, p, st);
-  else if (dtype == DT_FP16) head_dim == 64 ? bwd_general<f16_t, 64>(s, p, st) : bwd_general<f16_t, 128>(s, p, st);
-  else head_dim == 64 ? bwd_general<bf16_t, 64>(s, p, st) : bwd_general<bf16_t, 128>(s, p, st);
+  if (dtype != DT_FP32) launch_cross_tiles_bwd(dtype == DT_FP16, head_dim, s, p, st);
+  else head_dim == 64 ? bwd_f32<64>(s, p, st) : bwd_f32<128>(s, p, st);
 }
 
 }  // namespace slapo

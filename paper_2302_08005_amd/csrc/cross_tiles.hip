@@ -1,0 +1,940 @@
+// Cross attention on 16-bit types. The arrangement of the self-attention kernels: all products on v_mfma_f32_32x32x16, "transposed"
+// (S^T = K Q^T, O^T = V^T P^T, ...), so that the accumulators of the scores are the operand of the next product as they are, and the softmax
+// state of a row is one scalar per lane. Sums, softmax statistics and scores are 32-bit; the probabilities, and the gradients of the scores, are
+// rounded to the storage type where a matrix product takes them.
+//
+// A block of four wavefronts owns 128 / G rows of a (sample, key head): queries of all the heads that share the key head (CrossRows), or
+// states for dK/dV. Each wavefront owns 32 rows; G groups of wavefronts own the same rows and take every G-th 64-row tile of the other
+// sequence. Tiles come into two LDS stages by direct loads; what lies behind the visible states is out of the loads' bounds and arrives as zeros.
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_tile.h"
+#include "cross_attention.h"
+
+namespace slapo {
+
+namespace {
+
+struct CrossBlock { int x, head, split; };   // head: of all samples' key heads
+// Blocks are handed to the 8 XCDs round-robin in launch order; those of one head are renumbered to sit on one XCD next to each other in time, and
+// share the tiles through its L2.
+__device__ __forceinline__ CrossBlock cross_block(unsigned w, unsigned total, int nx, int splits) {
+  const unsigned xcd = w & 7, q = total >> 3, r = total & 7;
+  w = xcd * q + (xcd < r ? xcd : r) + (w >> 3);
+  CrossBlock id;
+  id.x = w % nx;
+  w /= nx;
+  id.split = w % splits;
+  id.head = w / splits;
+  return id;
+}
+// tiles of a split: the walk cut evenly
+__device__ __forceinline__ int split_begin(int n_tiles, int split, int splits) { return (int)((int64_t)n_tiles * split / splits); }
+
+// 64-row tiles of an operand whose rows are an even stride apart (states).
+template <int D>
+struct StateTiles {
+  static constexpr int SPR = D / 8, MINE = SPR / 4;
+  unsigned voff[MINE], bytes, step;
+  const bf16_t* base;
+  int wave;
+  // `rows` rows exist from base on
+  __device__ __forceinline__ StateTiles(const bf16_t* base, int64_t stride, int rows, int lane, int wave) : base(base), wave(wave) {
+    bytes = rows > 0 ? (unsigned)(((int64_t)(rows - 1) * stride + D) * 2) : 0u;
+    step = (unsigned)(64 * stride * 2);
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+      const int slot = (wave + 4 * k) * 64 + lane, row = slot / SPR, pos = slot % SPR;
+      voff[k] = (unsigned)(row * stride * 2) + (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
+    }
+  }
+  __device__ __forceinline__ void issue(bf16_t* tile, int t) const {
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) buffer_load_lds_16_untracked(base, bytes, tile + (wave + 4 * k) * 512, voff[k] + (unsigned)t * step, 0);
+  }
+};
+// 64-row tiles of two operands whose rows are CrossRows (queries and the gradients of their outputs), one tile after the other.
+template <int D>
+struct QueryTiles {
+  static constexpr int SPR = D / 8, MINE = SPR / 4;
+  unsigned qoff[MINE], ooff[MINE], qbytes, obytes, qstep, ostep, qcarry, ocarry;
+  int head[MINE], group, hstep, wave;
+  const bf16_t *q, *o;
+  __device__ __forceinline__ QueryTiles(const CrossRows& rows, const bf16_t* q, int64_t q_stride, const bf16_t* o, int64_t o_stride, int row0, int lane, int wave)
+      : group(rows.group), wave(wave), q(q), o(o) {
+    const int w = rows.group * D, tokens = 64 / rows.group;
+    hstep = 64 - tokens * rows.group;
+    qbytes = (unsigned)(((int64_t)(rows.q_len - 1) * q_stride + w) * 2);
+    obytes = (unsigned)(((int64_t)(rows.q_len - 1) * o_stride + w) * 2);
+    qstep = (unsigned)((tokens * q_stride + hstep * D) * 2);
+    ostep = (unsigned)((tokens * o_stride + hstep * D) * 2);
+    qcarry = (unsigned)((q_stride - w) * 2);   // from the last head of a token to the first of the next
+    ocarry = (unsigned)((o_stride - w) * 2);
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+      const int slot = (wave + 4 * k) * 64 + lane, row = slot / SPR, pos = slot % SPR, t = rows.token(row0 + row);
+      const unsigned chunk = (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
+      head[k] = row0 + row - t * rows.group;
+      qoff[k] = (unsigned)((t * q_stride + head[k] * D) * 2) + chunk;
+      ooff[k] = (unsigned)((t * o_stride + head[k] * D) * 2) + chunk;
+    }
+  }
+  __device__ __forceinline__ void issue(bf16_t* qtile, bf16_t* otile) {
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+      buffer_load_lds_16_untracked(q, qbytes, qtile + (wave + 4 * k) * 512, qoff[k], 0);
+      buffer_load_lds_16_untracked(o, obytes, otile + (wave + 4 * k) * 512, ooff[k], 0);
+    }
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {   // 64 rows on
+      head[k] += hstep;
+      const bool carry = head[k] >= group;
+      head[k] -= carry ? group : 0;
+      qoff[k] += qstep + (carry ? qcarry : 0u);
+      ooff[k] += ostep + (carry ? ocarry : 0u);
+    }
+  }
+};
+
+// A wavefront's 32 rows of output, [32][D] in its accumulators, on their way out through LDS, so that whole rows are stored (8 bytes of a lane at a
+// time join those of its neighbours). value(t, e): column 32 t + 8 (e / 4) + 4 (lane / 32) + e % 4 of row lane % 32; address(r): where row r
+// of the 32 starts; `rows` of them exist.
+template <int D, bool F16>
+struct RowStage {
+  static constexpr int P = D + 4, ELEMS = 32 * P;
+  static __device__ __forceinline__ void meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  template <class Value, class Address>
+  static __device__ __forceinline__ void store(bf16_t* stage, int lane, int rows, Value&& value, Address&& address) {
+    const int row = lane & 31, col = 4 * (lane >> 5);
+    meet();
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint2*>(stage + row * P + t * 32 + g * 8 + col) =
+            make_uint2(pack2<F16>(value(t, 4 * g), value(t, 4 * g + 1)), pack2<F16>(value(t, 4 * g + 2), value(t, 4 * g + 3)));
+    meet();
+    constexpr int CPR = D / 8, RPI = 64 / CPR;   // 16-byte chunks per row, rows per access
+    const int c = (lane % CPR) * 8;
+#pragma unroll 1
+    for (int r = lane / CPR; r < rows; r += RPI) {
+      const uint2* p = reinterpret_cast<const uint2*>(stage + r * P + c);
+      const uint2 w0 = p[0], w1 = p[1];
+      *reinterpret_cast<uint4*>(address(r) + c) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+    }
+  }
+};
+// The same rows as 32-bit values, packed [row][D] from `out` on.
+template <int D, class Value>
+__device__ __forceinline__ void store_part(float* out, int lane, int rows, Value&& value) {
+  const int row = lane & 31;
+  if (row >= rows) return;
+  float* p = out + row * D + 4 * (lane >> 5);
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4*>(p + t * 32 + g * 8) = make_float4(value(t, 4 * g), value(t, 4 * g + 1), value(t, 4 * g + 2), value(t, 4 * g + 3));
+}
+
+template <int N>
+__device__ __forceinline__ void zero(f32x16_t (&v)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[t][r] = 0.f;
+}
+
+// Running softmax of a row (a lane holds half of it) and the output accumulated under it.
+template <int D>
+struct Softmax {
+  static constexpr int NT = D / 32;
+  f32x16_t o[NT];
+  float m = -INFINITY, l = 0.f;   // maximum (raw scores), sum of this lane's half
+  __device__ __forceinline__ Softmax() { zero(o); }
+  // 32-row sub-tiles of scores -> probabilities against the new maximum; the rest is scaled down where it grew
+  template <int SUBS>
+  __device__ __forceinline__ void add(f32x16_t (&sc)[SUBS], float sl2) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < SUBS; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[i][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m, mx);
+    if (__any(m_new > m)) {
+      const float al = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * sl2);
+      l *= al;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= al;
+      m = m_new;
+    }
+    const float mb = m == -INFINITY ? 0.f : m * sl2;
+#pragma unroll
+    for (int i = 0; i < SUBS; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[i][r], sl2, -mb));
+        sc[i][r] = p;
+        l += p;
+      }
+  }
+  // what another wavefront has for the same rows and other states
+  template <class Other>
+  __device__ __forceinline__ void join(float m2, float l2, float sl2, Other&& o2) {
+    const float m_new = fmaxf(m, m2);
+    const float mine = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * sl2);
+    const float theirs = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - m_new) * sl2);
+    l = l * mine + l2 * theirs;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = o[t][r] * mine + o2(t, r) * theirs;
+    m = m_new;
+  }
+};
+
+// (a sum of 0: no state was seen; one that is no number stays so)
+__device__ __forceinline__ float inverse(float l) { return l != 0.f ? 1.f / l : 0.f; }
+__device__ __forceinline__ float log_sum(float m, float l, float scale) { return l != 0.f ? m * scale + __logf(l) : -INFINITY; }
+
+// Where forward's splits leave their outputs (32 bits, normalised over their own states) and logsumexps: [head][split][row][D], [head][split][row].
+struct FwdParts {
+  float *o, *lse;
+  int splits;
+  template <int D>
+  __device__ __forceinline__ float* rows(int head, int split, int64_t n_rows, int64_t r) const { return o + (((int64_t)head * splits + split) * n_rows + r) * D; }
+  __device__ __forceinline__ float* stat(int head, int split, int64_t n_rows, int64_t r) const { return lse + ((int64_t)head * splits + split) * n_rows + r; }
+};
+
+// =================================== forward: 128 / G rows per block ===================================
+template <int D, bool F16, int G>
+__global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOperands p, int nx, FwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // [2][G][K tile | V tile]
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits);
+  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
+  const CrossRows rows(sh);
+  const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), all_tiles = (n_keys + 63) / 64;
+  const int first = split_begin(all_tiles, blk.split, parts.splits), n_tiles = split_begin(all_tiles, blk.split + 1, parts.splits) - first;
+  const int wave_row = blk.x * RB + 32 * row_wave, my_row = wave_row + (lane & 31);
+  const int64_t head0 = (int64_t)h * sh.group * D;
+  const float sl2 = LOG2E * sh.scale;
+
+  const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
+  bf16x8_t qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(q + 16 * s + 8 * kc);
+  Softmax<D> sm;
+
+  const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const StateTiles<D> kt((const bf16_t*)p.k + kv0, sh.kv_stride, n_keys, lane, wave), vt((const bf16_t*)p.v + kv0, sh.kv_stride, n_keys, lane, wave);
+  auto issue_step = [&](int stage, int step) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int t = step * G + g;
+      if (t >= n_tiles) break;   // uniform
+      kt.issue(smem + (stage * G + g) * 2 * TE, first + t);
+      vt.issue(smem + (stage * G + g) * 2 * TE + TE, first + t);
+    }
+  };
+  auto compute = [&](int stage, int step) {
+    const int t = step * G + grp, kv0 = (first + t) * 64;
+    if (G > 1 && t >= n_tiles) return;
+    const bf16_t* ktile = smem + (stage * G + grp) * 2 * TE;
+    const bf16_t* vtile = ktile + TE;
+    f32x16_t sc[2];
+    zero(sc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) sc[i] = mfma16<F16>(frag_rows<D>(ktile, fr_base, i * 32, s), qf[s], sc[i]);
+    if (kv0 + 64 > n_keys) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[i][r] = kv0 + i * 32 + acc_row(r, lane) >= n_keys ? -INFINITY : sc[i][r];
+    }
+    sm.add(sc, sl2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const bf16x8_t pf = pack8<F16>(sc[i], half);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sm.o[t] = mfma16<F16>(frag_tr<D>(vtile, ft_base, i * 32 + 16 * half, t), pf, sm.o[t]);
+      }
+  };
+  tile_ring<2, G * 2 * StateTiles<D>::MINE>((n_tiles + G - 1) / G, issue_step, compute);
+  if constexpr (G > 1) {   // (the ring ends behind a barrier: the stages are free)
+    constexpr int REGS = NT * 16 + 2;
+    if (grp > 0) {
+      float* s = group_slot<G, REGS>(smem, grp, row_wave, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[(t * 16 + r) * 64] = sm.o[t][r];
+      s[NT * 16 * 64] = sm.m;
+      s[(NT * 16 + 1) * 64] = sm.l;
+    }
+    __syncthreads();
+    if (grp > 0) return;
+    for (int g = 1; g < G; ++g) {
+      const float* s = group_slot<G, REGS>(smem, g, row_wave, lane);
+      sm.join(s[NT * 16 * 64], s[(NT * 16 + 1) * 64], sl2, [&](int t, int r) { return s[(t * 16 + r) * 64]; });
+    }
+  }
+  const float l = sm.l + __shfl_xor(sm.l, 32, 64), inv = inverse(l);
+  if (wave_row >= n_rows) return;
+  const auto value = [&](int t, int e) { return sm.o[t][e] * inv; };
+  const float my_lse = log_sum(sm.m, l, sh.scale);
+  if (parts.splits > 1) {
+    store_part<D>(parts.rows<D>(blk.head, blk.split, n_rows, wave_row), lane, n_rows - wave_row, value);
+    if (kc == 0 && my_row < n_rows) *parts.stat(blk.head, blk.split, n_rows, my_row) = my_lse;
+    return;
+  }
+  bf16_t* out = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0;
+  // (a group's wavefront writes over its own slot of what the groups handed it)
+  bf16_t* stage = smem + row_wave * (G > 1 ? (NT * 16 + 2) * 128 : RowStage<D, F16>::ELEMS);
+  RowStage<D, F16>::store(stage, lane, min(32, n_rows - wave_row), value, [&](int r) { return out + rows.at(wave_row + r, sh.out_stride, D); });
+  if (p.lse && kc == 0 && my_row < n_rows) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(my_row)] = my_lse;
+}
+
+// ================================ forward: at most 32 rows of a head ====================================
+// A token or a few that are being generated: one wavefront has all rows, and the walk over the states is all there is to share. Bound by
+// reading them, so every wavefront walks tiles of 32 states of its own, NSTG of them on their way, and waits for nobody; its four
+// wavefronts' results meet in LDS, those of several blocks in a second kernel.
+template <int D> constexpr int FEW_STAGES = D == 64 ? 4 : 2;
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void cross_few_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, TE = 32 * D, NSTG = FEW_STAGES<D>, SPR = D / 8, LOADS = SPR / 2;   // wave-level loads per tile of 32 rows
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // per wavefront [NSTG][K tile | V tile]
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, 1, parts.splits);
+  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
+  const CrossRows rows(sh);
+  const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), all_tiles = (n_keys + 31) / 32;
+  const int first = split_begin(all_tiles, blk.split, parts.splits) + wave, end = split_begin(all_tiles, blk.split + 1, parts.splits);
+  const int n_tiles = first < end ? (end - first + 3) / 4 : 0;   // this wavefront's: every fourth
+  const int my_row = lane & 31;
+  const int64_t head0 = (int64_t)h * sh.group * D;
+  const float sl2 = LOG2E * sh.scale;
+  const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
+  bf16x8_t qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(q + 16 * s + 8 * kc);
+  Softmax<D> sm;
+
+  bf16_t* mine = smem + wave * NSTG * 2 * TE;
+  const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const bf16_t *k = (const bf16_t*)p.k + kv0, *v = (const bf16_t*)p.v + kv0;
+  const unsigned bytes = n_keys > 0 ? (unsigned)(((int64_t)(n_keys - 1) * sh.kv_stride + D) * 2) : 0u, step = (unsigned)(32 * sh.kv_stride * 2);
+  unsigned voff[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int slot = i * 64 + lane, row = slot / SPR, pos = slot % SPR;
+    voff[i] = (unsigned)(row * sh.kv_stride * 2) + (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
+  }
+  auto issue = [&](int stage, int i) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wavefront has read of the stage has arrived
+    const unsigned at = (unsigned)(first + 4 * i) * step;
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(k, bytes, mine + stage * 2 * TE + n * 512, voff[n] + at, 0);
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(v, bytes, mine + stage * 2 * TE + TE + n * 512, voff[n] + at, 0);
+  };
+  auto compute = [&](int stage, int i) {
+    const int key0 = (first + 4 * i) * 32;
+    const bf16_t *ktile = mine + stage * 2 * TE, *vtile = ktile + TE;
+    f32x16_t sc[1];
+    zero(sc);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) sc[0] = mfma16<F16>(frag_rows<D>(ktile, fr_base, 0, s), qf[s], sc[0]);
+    if (key0 + 32 > n_keys) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[0][r] = key0 + acc_row(r, lane) >= n_keys ? -INFINITY : sc[0][r];
+    }
+    sm.add(sc, sl2);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8_t pf = pack8<F16>(sc[0], half);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sm.o[t] = mfma16<F16>(frag_tr<D>(vtile, ft_base, 16 * half, t), pf, sm.o[t]);
+    }
+  };
+  // the tile that is computed next has landed when at most the younger ones' loads are outstanding
+  auto wait_for_oldest = [&](int younger) {
+    if (younger >= 3 && NSTG > 3) wait_loads_and_lds<(NSTG > 3 ? 3 : 0) * 2 * LOADS>();
+    else if (younger == 2 && NSTG > 2) wait_loads_and_lds<(NSTG > 2 ? 2 : 0) * 2 * LOADS>();
+    else if (younger == 1) wait_loads_and_lds<2 * LOADS>();
+    else wait_loads_and_lds<0>();
+    asm volatile("" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < NSTG - 1; ++i)
+    if (i < n_tiles) issue(i, i);
+  for (int i0 = 0; i0 < n_tiles; i0 += NSTG) {
+#pragma unroll
+    for (int s = 0; s < NSTG; ++s) {
+      const int i = i0 + s;
+      if (i >= n_tiles) break;   // uniform
+      if (i + NSTG - 1 < n_tiles) issue((s + NSTG - 1) % NSTG, i + NSTG - 1);   // (that stage's reads have been used)
+      wait_for_oldest(min(NSTG - 1, n_tiles - 1 - i));
+      compute(s, i);
+    }
+  }
+  // wavefront w puts together columns 32 w .. of all four
+  __syncthreads();
+  constexpr int REGS = NT * 16 + 2;
+  float* slots = reinterpret_cast<float*>(smem);
+  {
+    float* s = slots + wave * REGS * 64 + lane;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[(t * 16 + r) * 64] = sm.o[t][r];
+    s[NT * 16 * 64] = sm.m;
+    s[(NT * 16 + 1) * 64] = sm.l + __shfl_xor(sm.l, 32, 64);
+  }
+  __syncthreads();
+  if (wave >= NT) return;
+  float m = -INFINITY, l = 0.f, weight[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m = fmaxf(m, slots[(w * REGS + NT * 16) * 64 + lane]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    weight[w] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((slots[(w * REGS + NT * 16) * 64 + lane] - m) * sl2);
+    l += weight[w] * slots[(w * REGS + NT * 16 + 1) * 64 + lane];
+  }
+  const float inv = inverse(l);
+  if (my_row >= n_rows) return;
+  float o[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    o[r] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) o[r] += weight[w] * slots[(w * REGS + wave * 16 + r) * 64 + lane];
+    o[r] *= inv;
+  }
+  const float my_lse = log_sum(m, l, sh.scale);
+  const int col = wave * 32 + 4 * kc;
+  if (parts.splits > 1) {
+    float* dst = parts.rows<D>(blk.head, blk.split, n_rows, my_row) + col;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(dst + 8 * g) = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+    if (wave == 0 && kc == 0) *parts.stat(blk.head, blk.split, n_rows, my_row) = my_lse;
+  } else {
+    bf16_t* dst = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(my_row, sh.out_stride, D) + col;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *reinterpret_cast<uint2*>(dst + 8 * g) = make_uint2(pack2<F16>(o[4 * g], o[4 * g + 1]), pack2<F16>(o[4 * g + 2], o[4 * g + 3]));
+    if (p.lse && wave == 0 && kc == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(my_row)] = my_lse;
+  }
+}
+
+// Puts the splits of a row together, by their logsumexps: a wavefront per row.
+constexpr int MAX_SPLITS = 64;
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
+  const CrossRows rows(sh);
+  const int n_rows = rows.count(), lane = threadIdx.x & 63;
+  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (item >= (int64_t)sh.batch * sh.kv_heads * n_rows) return;
+  const int head = (int)(item / n_rows), r = (int)(item - (int64_t)head * n_rows), b = head / sh.kv_heads, h = head - b * sh.kv_heads;
+  const float lse = lane < parts.splits ? *parts.stat(head, lane, n_rows, r) : -INFINITY;
+  const float m = wave_max(lse), base = m == -INFINITY ? 0.f : m;
+  const float e = __expf(lse - base), total = wave_sum(e), weight = e * inverse(total);
+  constexpr int C = D / 64;
+  float o[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) o[c] = 0.f;
+  for (int s = 0; s < parts.splits; ++s) {
+    const float w = __shfl(weight, s, 64);
+    const float* src = parts.rows<D>(head, s, n_rows, r) + C * lane;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = fmaf(w, src[c], o[c]);
+  }
+  bf16_t* dst = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + (int64_t)h * sh.group * D + rows.at(r, sh.out_stride, D) + C * lane;
+  if constexpr (C == 2) *reinterpret_cast<uint32_t*>(dst) = pack2<F16>(o[0], o[1]);
+  else *dst = (bf16_t)(pack2<F16>(o[0], 0.f) & 0xffffu);
+  if (p.lse && lane == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(r)] = total != 0.f ? base + __logf(total) : -INFINITY;
+}
+
+// ======================================== backward ======================================================
+// 32-bit parts of gradients that several blocks share: [part][head][array][row][D].
+struct BwdParts {
+  float* o;
+  int splits;
+  template <int D>
+  __device__ __forceinline__ float* rows(int head, int heads, int split, int arrays, int array, int64_t n_rows, int64_t r) const {
+    return o + ((((int64_t)split * heads + head) * arrays + array) * n_rows + r) * D;
+  }
+};
+
+// dQ of 128 / G rows. Also leaves delta = rowsum(dO * O) of its rows, laid out as lse, for the kernel of dK and dV.
+template <int D, bool F16, int G>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 1) void cross_dq_kernel(CrossShape sh, CrossOperands p, int nx, float* __restrict__ delta, BwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // [2][G][K tile | V tile]
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits);
+  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
+  const CrossRows rows(sh);
+  const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), all_tiles = (n_keys + 63) / 64;
+  const int first = split_begin(all_tiles, blk.split, parts.splits), n_tiles = split_begin(all_tiles, blk.split + 1, parts.splits) - first;
+  const int wave_row = blk.x * RB + 32 * row_wave, my_row = wave_row + (lane & 31), ld_row = min(my_row, n_rows - 1);
+  const int64_t head0 = (int64_t)h * sh.group * D, stat = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(ld_row);
+  const float sl2 = LOG2E * sh.scale;
+
+  const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(ld_row, sh.q_stride, D);
+  const int64_t out0 = (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(ld_row, sh.out_stride, D);
+  bf16x8_t qf[NS], df[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    qf[s] = *reinterpret_cast<const bf16x8_t*>(q + 16 * s + 8 * kc);
+    df[s] = *reinterpret_cast<const bf16x8_t*>((const bf16_t*)p.dout + out0 + 16 * s + 8 * kc);
+  }
+  const float my_lse2 = p.lse[stat] * LOG2E;
+  // the lane holds half of the row's dO, lane ^ 32 the other half
+  float my_delta = 0.f;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const bf16x8_t of = *reinterpret_cast<const bf16x8_t*>((const bf16_t*)p.out + out0 + 16 * s + 8 * kc);
+    const u32x4_t ow = __builtin_bit_cast(u32x4_t, of), dw = __builtin_bit_cast(u32x4_t, df[s]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      my_delta = fmaf(unpack_lo<F16>(ow[e]), unpack_lo<F16>(dw[e]), my_delta);
+      my_delta = fmaf(unpack_hi<F16>(ow[e]), unpack_hi<F16>(dw[e]), my_delta);
+    }
+  }
+  my_delta += __shfl_xor(my_delta, 32, 64);
+  f32x16_t dq[NT];
+  zero(dq);
+
+  const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const StateTiles<D> kt((const bf16_t*)p.k + kv0, sh.kv_stride, n_keys, lane, wave), vt((const bf16_t*)p.v + kv0, sh.kv_stride, n_keys, lane, wave);
+  auto issue_step = [&](int stage, int step) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int t = step * G + g;
+      if (t >= n_tiles) break;   // uniform
+      kt.issue(smem + (stage * G + g) * 2 * TE, first + t);
+      vt.issue(smem + (stage * G + g) * 2 * TE + TE, first + t);
+    }
+  };
+  // probabilities and their gradients of 32 states
+  auto scores = [&](const bf16_t* ktile, const bf16_t* vtile, int i, int kv0, f32x16_t& sc, f32x16_t& dp) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      sc = mfma16<F16>(frag_rows<D>(ktile, fr_base, i * 32, s), qf[s], sc);
+      dp = mfma16<F16>(frag_rows<D>(vtile, fr_base, i * 32, s), df[s], dp);
+    }
+    auto elements = [&](auto edge) {   // (two instances: interior tiles carry no mask code)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], sl2, -my_lse2));
+        if (decltype(edge)::value) sc[r] = kv0 + i * 32 + acc_row(r, lane) >= n_keys ? 0.f : sc[r];
+      }
+    };
+    if (kv0 + 64 > n_keys) elements(std::true_type{});
+    else elements(std::false_type{});
+  };
+  auto compute = [&](int stage, int step) {
+    const int t = step * G + grp, kv0 = (first + t) * 64;
+    if (G > 1 && t >= n_tiles) return;
+    const bf16_t* ktile = smem + (stage * G + grp) * 2 * TE;
+    const bf16_t* vtile = ktile + TE;
+    if (all_tiles == 1) {
+      // All states of the sample are here: delta as sum p dP, without the rounding of O. With few states the gradient of a score is a
+      // small difference (none at all with one), where that rounding would show.
+      my_delta = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        f32x16_t sc, dp;
+        scores(ktile, vtile, i, kv0, sc, dp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) my_delta = fmaf(sc[r], dp[r], my_delta);
+      }
+      my_delta += __shfl_xor(my_delta, 32, 64);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f32x16_t sc, dp;
+      scores(ktile, vtile, i, kv0, sc, dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - my_delta);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const bf16x8_t dsf = pack8<F16>(dp, half);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) dq[t] = mfma16<F16>(frag_tr<D>(ktile, ft_base, i * 32 + 16 * half, t), dsf, dq[t]);
+      }
+    }
+  };
+  tile_ring<2, G * 2 * StateTiles<D>::MINE>((n_tiles + G - 1) / G, issue_step, compute);
+  // (group 0 of the last split has the tile of a walk that is one)
+  if (grp == 0 && blk.split == parts.splits - 1 && kc == 0 && my_row < n_rows) delta[stat] = my_delta;
+  if constexpr (G > 1) {
+    constexpr int REGS = NT * 16;
+    if (grp > 0) {
+      float* s = group_slot<G, REGS>(smem, grp, row_wave, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[(t * 16 + r) * 64] = dq[t][r];
+    }
+    __syncthreads();
+    if (grp > 0) return;
+    for (int g = 1; g < G; ++g) {
+      const float* s = group_slot<G, REGS>(smem, g, row_wave, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[t][r] += s[(t * 16 + r) * 64];
+    }
+  }
+  if (wave_row >= n_rows) return;
+  const auto value = [&](int t, int e) { return dq[t][e] * sh.scale; };
+  if (parts.splits > 1) {
+    store_part<D>(parts.rows<D>(blk.head, sh.batch * sh.kv_heads, blk.split, 1, 0, n_rows, wave_row), lane, n_rows - wave_row, value);
+    return;
+  }
+  bf16_t* out = (bf16_t*)p.dq + (int64_t)b * sh.q_len * sh.q_stride + head0;
+  bf16_t* stage = smem + row_wave * (G > 1 ? NT * 16 * 128 : RowStage<D, F16>::ELEMS);
+  RowStage<D, F16>::store(stage, lane, min(32, n_rows - wave_row), value, [&](int r) { return out + rows.at(wave_row + r, sh.q_stride, D); });
+}
+
+// dK and dV of 128 / G states; those of hidden states are zeros.
+template <int D, bool F16, int G>
+__global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_kernel(CrossShape sh, CrossOperands p, int nx, const float* __restrict__ delta, BwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
+  constexpr int TILE = 2 * TE + 256;    // 16-bit units: Q tile, dO tile, 64 lse + 64 delta floats
+  constexpr int STAGE = G * TILE;
+  constexpr int FB = 4;                 // k-steps of fragment prefetch
+  constexpr bool ACC_A = D == 128;      // dK/dV accumulators in AGPRs (see mfma16_agpr)
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits);
+  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
+  const CrossRows rows(sh);
+  const int kv_base = blk.x * RB, n_keys = visible(sh, p.lens, b), n_rows = rows.count();
+  const int all_tiles = kv_base < n_keys ? (n_rows + 63) / 64 : 0;   // nothing to do for hidden states
+  const int first = split_begin(all_tiles, blk.split, parts.splits), n_tiles = split_begin(all_tiles, blk.split + 1, parts.splits) - first;
+  const int wave_key = kv_base + 32 * row_wave, my_key = wave_key + (lane & 31);
+  const bool seen = my_key < n_keys, key_edge = wave_key + 32 > n_keys;
+  const int64_t head0 = (int64_t)h * sh.group * D, stats0 = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
+  const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const float sl2 = LOG2E * sh.scale;
+
+  bf16x8_t kf[NS], vf[NS];
+  {
+    const int64_t at = kv0 + (int64_t)min(my_key, sh.kv_len - 1) * sh.kv_stride + 8 * kc;
+    const bf16x8_t none = {};
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      kf[s] = seen ? *reinterpret_cast<const bf16x8_t*>((const bf16_t*)p.k + at + 16 * s) : none;
+      vf[s] = seen ? *reinterpret_cast<const bf16x8_t*>((const bf16_t*)p.v + at + 16 * s) : none;
+    }
+  }
+  f32x16_t dk[NT], dv[NT];
+  zero(dk);
+  zero(dv);
+
+  // threads 0..63 carry lse, threads 64..127 delta, threads 128..255 duplicate them or bring the second tile of a step
+  const float* stat_src = ((tid & 127) < 64 ? p.lse : delta) + stats0;
+  const float stat_mul = (tid & 127) < 64 ? LOG2E : 1.0f;
+  const int stat_tile = (tid >> 7) % G;
+  auto load_stats = [&](int step) { return stat_src[rows.stat(min((first + step * G + stat_tile) * 64 + (tid & 63), n_rows - 1))]; };
+  auto store_stats = [&](int stage, float v) { reinterpret_cast<float*>(smem + stage * STAGE + stat_tile * TILE + 2 * TE)[tid & 127] = v * stat_mul; };
+  QueryTiles<D> tiles(rows, (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0, sh.q_stride,
+                      (const bf16_t*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0, sh.out_stride, first * 64, lane, wave);
+  auto issue_step = [&](int stage, int step) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (step * G + g >= n_tiles) break;   // uniform
+      tiles.issue(smem + stage * STAGE + g * TILE, smem + stage * STAGE + g * TILE + TE);
+    }
+  };
+  auto compute = [&](int stage, int step) {
+    if (G > 1 && step * G + grp >= n_tiles) return;
+    const int q0 = (first + step * G + grp) * 64;
+    const bf16_t* qtile = smem + stage * STAGE + grp * TILE;
+    const bf16_t* dtile = qtile + TE;
+    const float* stat = reinterpret_cast<const float*>(qtile + 2 * TE);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int qs = q0 + i * 32;
+      f32x16_t sc, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = dp[r] = 0.f;
+      // Fragments are requested FB k-steps ahead of the MFMAs that use them and the order is pinned: left to itself the scheduler
+      // reuses one register set for all fragments, and every MFMA then waits out the LDS latency of its own read.
+#pragma unroll
+      for (int s0 = 0; s0 < NS; s0 += FB) {
+        bf16x8_t fq[FB], fd[FB];
+#pragma unroll
+        for (int s = 0; s < FB; ++s) {
+          fq[s] = frag_rows<D>(qtile, fr_base, i * 32, s0 + s);
+          fd[s] = frag_rows<D>(dtile, fr_base, i * 32, s0 + s);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < FB; ++s) {
+          sc = mfma16<F16>(fq[s], kf[s0 + s], sc);
+          dp = mfma16<F16>(fd[s], vf[s0 + s], dp);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // the first operands of the dV / dK products do not depend on the softmax: on their way during it
+      bf16x8_t td0[NT], tq0[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        td0[t] = frag_tr<D>(dtile, ft_base, i * 32, t);
+        tq0[t] = frag_tr<D>(qtile, ft_base, i * 32, t);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      auto elements = [&](auto edge) {   // (two instances: interior tiles carry no mask code)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 l4 = *reinterpret_cast<const float4*>(stat + i * 32 + g * 8 + 4 * kc);
+          const float4 d4 = *reinterpret_cast<const float4*>(stat + 64 + i * 32 + g * 8 + 4 * kc);
+          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * g + e;
+            float pr = __builtin_amdgcn_exp2f(fmaf(sc[r], sl2, -ls[e]));
+            if (decltype(edge)::value) pr = (!seen | (qs + g * 8 + 4 * kc + e >= n_rows)) ? 0.f : pr;
+            sc[r] = pr;
+            dp[r] = pr * (dp[r] - ds[e]);
+          }
+        }
+      };
+      if (key_edge || qs + 32 > n_rows) elements(std::true_type{});
+      else elements(std::false_type{});
+      const bf16x8_t pf0 = pack8<F16>(sc, 0), dsf0 = pack8<F16>(dp, 0), pf1 = pack8<F16>(sc, 1), dsf1 = pack8<F16>(dp, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      bf16x8_t td1[NT], tq1[NT];   // second half's operands, requested in front of the first half's MFMAs
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        td1[t] = frag_tr<D>(dtile, ft_base, i * 32 + 16, t);
+        tq1[t] = frag_tr<D>(qtile, ft_base, i * 32 + 16, t);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if constexpr (ACC_A) { mfma16_agpr<F16>(dv[t], td0[t], pf0); mfma16_agpr<F16>(dk[t], tq0[t], dsf0); }
+        else { dv[t] = mfma16<F16>(td0[t], pf0, dv[t]); dk[t] = mfma16<F16>(tq0[t], dsf0, dk[t]); }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if constexpr (ACC_A) { mfma16_agpr<F16>(dv[t], td1[t], pf1); mfma16_agpr<F16>(dk[t], tq1[t], dsf1); }
+        else { dv[t] = mfma16<F16>(td1[t], pf1, dv[t]); dk[t] = mfma16<F16>(tq1[t], dsf1, dk[t]); }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Two stages: step it + 1 is requested while step it is computed; its statistics travel through registers and are requested before its tile
+  // loads, so that waiting for them leaves those in flight.
+  const int n_steps = (n_tiles + G - 1) / G;
+  if (n_steps > 0) {
+    const float stat0 = load_stats(0);
+    issue_step(0, 0);
+    store_stats(0, stat0);
+    wait_loads_and_lds<0>();
+    block_barrier();
+    for (int it0 = 0; it0 < n_steps; it0 += 2) {
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const int it = it0 + st;
+        if (it >= n_steps) break;   // uniform
+        const bool more = it + 1 < n_steps;
+        float next = 0.f;
+        if (more) {
+          next = load_stats(it + 1);
+          issue_step(st ^ 1, it + 1);
+        }
+        compute(st, it);
+        if (more) store_stats(st ^ 1, next);
+        wait_loads_and_lds<0>();
+        block_barrier();
+      }
+    }
+  }
+  if (ACC_A) agpr_results_ready();
+  if constexpr (G > 1) {   // (behind the last barrier: the stages are free)
+    constexpr int REGS = 2 * NT * 16;
+    if (grp > 0) {
+      float* s = group_slot<G, REGS>(smem, grp, row_wave, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { s[(t * 16 + r) * 64] = dk[t][r]; s[((NT + t) * 16 + r) * 64] = dv[t][r]; }
+    }
+    __syncthreads();
+    if (grp > 0) return;
+    for (int g = 1; g < G; ++g) {
+      const float* s = group_slot<G, REGS>(smem, g, row_wave, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { dk[t][r] += s[(t * 16 + r) * 64]; dv[t][r] += s[((NT + t) * 16 + r) * 64]; }
+    }
+  }
+  if (wave_key >= sh.kv_len) return;
+  const auto dk_value = [&](int t, int e) { return seen ? dk[t][e] * sh.scale : 0.f; };   // (a row whose gradient is no number must not reach a hidden state)
+  const auto dv_value = [&](int t, int e) { return seen ? dv[t][e] : 0.f; };
+  const int there = sh.kv_len - wave_key;
+  if (parts.splits > 1) {
+    store_part<D>(parts.rows<D>(blk.head, sh.batch * sh.kv_heads, blk.split, 2, 0, sh.kv_len, wave_key), lane, there, dk_value);
+    store_part<D>(parts.rows<D>(blk.head, sh.batch * sh.kv_heads, blk.split, 2, 1, sh.kv_len, wave_key), lane, there, dv_value);
+    return;
+  }
+  bf16_t* stage = smem + row_wave * (G > 1 ? 2 * NT * 16 * 128 : RowStage<D, F16>::ELEMS);
+  const int64_t at = kv0 + wave_key * sh.kv_stride;
+  RowStage<D, F16>::store(stage, lane, min(32, there), dk_value, [&](int r) { return (bf16_t*)p.dk + at + r * sh.kv_stride; });
+  RowStage<D, F16>::store(stage, lane, min(32, there), dv_value, [&](int r) { return (bf16_t*)p.dv + at + r * sh.kv_stride; });
+}
+
+// Adds up the parts of a gradient, in their order, eight columns per thread. QUERY: dq, rows of which are CrossRows; else dk and dv.
+template <int D, bool F16, bool QUERY>
+__global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
+  constexpr int C = D / 8, ARRAYS = QUERY ? 1 : 2;
+  const CrossRows rows(sh);
+  const int64_t n_rows = QUERY ? rows.count() : sh.kv_len, heads = (int64_t)sh.batch * sh.kv_heads, items = heads * ARRAYS * n_rows * C;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= items) return;
+  float v[8], w[8];
+  load8(parts.o + 8 * i, v);
+  for (int s = 1; s < parts.splits; ++s) {
+    load8(parts.o + 8 * (i + s * items), w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  const int c = (int)(i % C) * 8;
+  const int64_t row = i / C, r = row % n_rows, plane = row / n_rows, head = plane / ARRAYS, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
+  bf16_t* dst;
+  if (QUERY) dst = (bf16_t*)p.dq + b * sh.q_len * sh.q_stride + h * sh.group * D + rows.at((int)r, sh.q_stride, D);
+  else dst = (bf16_t*)(plane % ARRAYS ? p.dv : p.dk) + (b * sh.kv_len + r) * sh.kv_stride + h * D;
+  store8h<F16>(dst + c, v);
+}
+
+// ======================================== launches ======================================================
+// What a launch looks like: groups of wavefronts per block, blocks along the rows, splits of the walk.
+struct Form { int groups, nx, splits; };
+
+// `rows` own rows of each of `heads` heads, a walk of `walk` others
+Form form(int64_t rows, int64_t walk, int64_t heads) {
+  Form f;
+  const int64_t tiles = (walk + 63) / 64;
+  f.groups = ((rows + 63) / 64) * heads <= 256 && tiles > 1 ? 2 : 1;
+  f.nx = (int)((rows + 128 / f.groups - 1) / (128 / f.groups));
+  const int64_t blocks = f.nx * heads;
+  f.splits = 1;
+  while (f.splits < MAX_SPLITS && blocks * f.splits * 2 <= 256 && tiles >= 4 * f.groups * f.splits) f.splits *= 2;
+  return f;
+}
+constexpr int FEW_ROWS = 32;
+int few_splits(int64_t walk, int64_t heads) {
+  const int64_t tiles = (walk + 31) / 32;
+  int splits = 1;
+  while (splits < MAX_SPLITS && heads * splits * 2 <= 512 && tiles >= 8 * 2 * splits) splits *= 2;
+  return splits;
+}
+inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+struct FwdPlan { bool few; Form form; size_t o_bytes, total; };
+FwdPlan fwd_plan(int head_dim, const CrossShape& s) {
+  FwdPlan f;
+  const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
+  f.few = rows <= FEW_ROWS;
+  f.form = f.few ? Form{4, 1, few_splits(s.kv_len, heads)} : form(rows, s.kv_len, heads);
+  const size_t all = (size_t)(heads * rows * f.form.splits);
+  f.o_bytes = f.form.splits > 1 ? up256(all * head_dim * 4) : 0;
+  f.total = f.form.splits > 1 ? f.o_bytes + up256(all * 4) : 0;
+  return f;
+}
+struct BwdPlan { Form q, kv; size_t delta_bytes, dq_bytes, total; };   // the parts of dq and those of dk and dv share memory one after the other
+BwdPlan bwd_plan(int head_dim, const CrossShape& s) {
+  BwdPlan f;
+  const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
+  f.q = form(rows, s.kv_len, heads);
+  f.kv = form(s.kv_len, rows, heads);
+  f.delta_bytes = up256((size_t)(heads * rows) * 4);
+  const size_t dq = f.q.splits > 1 ? (size_t)(heads * rows * f.q.splits) * head_dim * 4 : 0;
+  const size_t dkv = f.kv.splits > 1 ? (size_t)(heads * s.kv_len * f.kv.splits) * 2 * head_dim * 4 : 0;
+  f.total = f.delta_bytes + up256(dq > dkv ? dq : dkv);
+  return f;
+}
+
+template <class Kernel, class... Args>
+void launch(Kernel kernel, int64_t blocks, size_t lds, hipStream_t st, Args... args) {
+  if (lds > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, st, args...);
+}
+
+template <int D, bool F16>
+void fwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
+  const FwdPlan f = fwd_plan(D, s);
+  const int64_t heads = (int64_t)s.batch * s.kv_heads, rows = (int64_t)s.q_len * s.group;
+  const FwdParts parts = {p.ws, (float*)((char*)p.ws + f.o_bytes), f.form.splits};
+  constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t);   // K and V
+  const int64_t blocks = heads * f.form.nx * f.form.splits;
+  if (f.few) launch(cross_few_kernel<D, F16>, blocks, FEW_STAGES<D> * 4 * tile / 2, st, s, p, parts);
+  else if (f.form.groups == 2) launch(cross_fwd_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.form.nx, parts);
+  else launch(cross_fwd_kernel<D, F16, 1>, blocks, std::max(2 * tile, (size_t)4 * RowStage<D, F16>::ELEMS * 2), st, s, p, f.form.nx, parts);
+  if (f.form.splits > 1) launch(cross_join_kernel<D, F16>, (heads * rows + 3) / 4, 0, st, s, p, parts);
+}
+
+template <int D, bool F16>
+void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
+  const BwdPlan f = bwd_plan(D, s);
+  const int64_t heads = (int64_t)s.batch * s.kv_heads, rows = (int64_t)s.q_len * s.group;
+  float *delta = p.ws, *memory = (float*)((char*)p.ws + f.delta_bytes);
+  constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t), rows_out = (size_t)4 * RowStage<D, F16>::ELEMS * 2;
+  {
+    const BwdParts parts = {memory, f.q.splits};
+    const int64_t blocks = heads * f.q.nx * f.q.splits;
+    if (f.q.groups == 2) launch(cross_dq_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.q.nx, delta, parts);
+    else launch(cross_dq_kernel<D, F16, 1>, blocks, std::max(2 * tile, rows_out), st, s, p, f.q.nx, delta, parts);
+    if (f.q.splits > 1) launch(cross_sum_kernel<D, F16, true>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts);
+  }
+  {
+    const BwdParts parts = {memory, f.kv.splits};
+    const int64_t blocks = heads * f.kv.nx * f.kv.splits;
+    constexpr size_t stage = tile + 512, meet = (size_t)2 * D * 2 * 64 * sizeof(float);   // two wavefronts' dK and dV
+    if (f.kv.groups == 2) launch(cross_dkdv_kernel<D, F16, 2>, blocks, std::max(4 * stage, meet), st, s, p, f.kv.nx, (const float*)delta, parts);
+    else launch(cross_dkdv_kernel<D, F16, 1>, blocks, std::max(2 * stage, rows_out), st, s, p, f.kv.nx, (const float*)delta, parts);
+    if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16, false>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
+  }
+}
+
+}  // namespace
+
+size_t cross_tiles_fwd_ws_bytes(int head_dim, const CrossShape& s) { return fwd_plan(head_dim, s).total; }
+size_t cross_tiles_bwd_ws_bytes(int head_dim, const CrossShape& s) { return bwd_plan(head_dim, s).total; }
+void launch_cross_tiles_fwd(bool f16, int head_dim, const CrossShape& s, const CrossOperands& p, hipStream_t st) {
+  if (f16) head_dim == 64 ? fwd<64, true>(s, p, st) : fwd<128, true>(s, p, st);
+  else head_dim == 64 ? fwd<64, false>(s, p, st) : fwd<128, false>(s, p, st);
+}
+void launch_cross_tiles_bwd(bool f16, int head_dim, const CrossShape& s, const CrossOperands& p, hipStream_t st) {
+  if (f16) head_dim == 64 ? bwd<64, true>(s, p, st) : bwd<128, true>(s, p, st);
+  else head_dim == 64 ? bwd<64, false>(s, p, st) : bwd<128, false>(s, p, st);
+}
+
+}  // namespace slapo

@@ -68,16 +68,15 @@ class Problem:
         q, k, v, do = self.host
         self.forward()
         out, lse = O.cross_forward(q, k, v, self.lens, self.scale)
-        stored = self.heads_of(self.out)
-        bounds = O.cross_bounds(q, k, v, do, self.lens, self.scale, stored, ROUND[self.dtype], TINY[self.dtype])
-        within(stored, out, bounds[0], "out")
+        bounds = O.cross_bounds(q, k, v, do, self.lens, self.scale, ROUND[self.dtype], TINY[self.dtype], 0 if self.dtype == W.FP32 else 64)
+        within(self.heads_of(self.out), out, bounds[0], "out")
         got = to_np(self.lse)
         assert np.array_equal(np.isneginf(got), np.isneginf(lse))
         seen = np.isfinite(lse)
         within(got[seen], lse[seen], bounds[1][seen], "lse")
         if backward:
             self.backward()
-            for name, want, bound in zip(("dq", "dk", "dv"), O.cross_backward(q, k, v, do, self.lens, self.scale, stored), bounds[2:]):
+            for name, want, bound in zip(("dq", "dk", "dv"), O.cross_backward(q, k, v, do, self.lens, self.scale), bounds[2:]):
                 within(self.heads_of(getattr(self, name)), want, bound, name)
         for back, w in ((self.out_back, self.out), (self.dq_back, self.dq)):   # columns between the rows are left alone
             gap = back[..., w.shape[-1]:]
