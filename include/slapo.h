@@ -335,21 +335,22 @@ typedef struct {
   int64_t q_stride, kv_stride, out_stride;  /* of q and dq; k, v, dk and dv; out and dout */
 } slapo_cross_attn_desc;
 
-/* Bytes of device workspace that forward and backward of this shape need (forward: may be 0, ws may then be NULL). A workspace serves
- * one call at a time and is free again when the call's work is done. */
+/* Bytes of device workspace that forward and backward of this shape need (forward: may be 0, ws may then be NULL; one that is too
+ * small is refused with SLAPO_ERR_WORKSPACE). A workspace serves one call at a time and is free again when the call's work is done. */
 int slapo_cross_attn_workspace(const slapo_cross_attn_desc *desc, size_t *fwd_bytes, size_t *bwd_bytes);
 
 /* kv_lens: device int32 [batch], visible states of each sample (values outside 0 .. kv_len count as the nearer end), or NULL: all.
  * What lies in the states behind them, infinities and NaN included, reaches no result. Where a sample has none, out is 0 and lse -infinity.
  * lse: fp32 [batch, heads, q_len] (natural log), which backward needs; may be NULL. out overlaps no input. */
 int slapo_cross_attn_fwd(const slapo_cross_attn_desc *desc, const void *q, const void *k, const void *v, const int32_t *kv_lens,
-                         void *out, float *lse, void *ws, void *stream);
+                         void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* Backward: dq, dk and dv from dout = dL/dout, the inputs, and the out and lse of the matching forward. dk and dv are summed over the query
  * heads that share a key head; those of hidden states, and all gradients of a sample without states, are 0. The gradients overlap neither
  * each other nor the inputs. */
 int slapo_cross_attn_bwd(const slapo_cross_attn_desc *desc, const void *q, const void *k, const void *v, const int32_t *kv_lens,
-                         const void *out, const void *dout, const float *lse, void *dq, void *dk, void *dv, void *ws, void *stream);
+                         const void *out, const void *dout, const float *lse, void *dq, void *dk, void *dv, void *ws,
+                         size_t ws_bytes, void *stream);
 
 /* Rotary embedding with positions of several axes (time, height and width of video tokens, rows and columns of an image's patches),
  * on the first `heads` heads of every row: queries and keys of a packed projection, or either of them alone. The pairs (2j, 2j+1) of a

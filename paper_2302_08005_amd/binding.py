@@ -96,8 +96,8 @@ def lib():
             "slapo_weight_grad": [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp],
             "slapo_weight_grad_static": [i32, i32, i64, i64, i64, vp, vp, vp, vp],
             "slapo_cross_attn_workspace": [C.POINTER(CrossAttnDesc), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
-            "slapo_cross_attn_fwd": [C.POINTER(CrossAttnDesc), vp, vp, vp, vp, vp, vp, vp, vp],
-            "slapo_cross_attn_bwd": [C.POINTER(CrossAttnDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp],
+            "slapo_cross_attn_fwd": [C.POINTER(CrossAttnDesc), vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp],
+            "slapo_cross_attn_bwd": [C.POINTER(CrossAttnDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp],
             "slapo_rope_axes": [C.POINTER(RopeAxesDesc), vp, vp, vp, i32, vp],
             "slapo_grad_plan_bytes": [i32, C.POINTER(_Grad), C.POINTER(C.c_size_t)],
             "slapo_grad_plan_build": [i32, C.POINTER(_Grad), vp, C.POINTER(_GradPlan), vp],
@@ -309,31 +309,29 @@ def _arg(name, t, dtype, shape, strides, device, optional=False):
     """Address of a tensor of exactly this kind."""
     if t is None and optional:
         return None
-    if t.dtype is not dtype or t.shape != shape or t.device.index != device or not t.is_cuda or t.stride() != strides:
-        # (the stride of a dimension of one element says nothing)
-        if t.dtype is dtype and t.shape == shape and t.is_cuda and t.device.index == device and \
-                all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), strides)):
-            return t.data_ptr()
+    # (the stride of a dimension of one element says nothing)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_cuda or \
+            (t.stride() != strides and not all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), strides))):
         _refuse(name, t, f"{dtype} of shape {tuple(shape)} with strides {tuple(strides)}")
     return t.data_ptr()
 
 
-def _room(name, t, nbytes, device):
-    """Address of a workspace."""
+def _room(t, device):
+    """Address and bytes of a workspace (the library knows how many it wants)."""
     if t is None:
-        if nbytes:
-            raise ValueError(f"{name}: a workspace of {nbytes} bytes is wanted")
-        return None
-    if not t.is_cuda or t.device.index != device or not t.is_contiguous() or t.numel() * t.element_size() < nbytes:
-        _refuse(name, t, f"{nbytes} contiguous bytes")
-    return t.data_ptr()
+        return None, 0
+    if not t.is_cuda or t.get_device() != device or not t.is_contiguous():
+        _refuse("ws", t, "a contiguous workspace")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _stream_and_device(stream):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    if s.device_index != torch.cuda.current_device():   # (kernels are launched on the current device)
-        raise ValueError(f"the stream belongs to device {s.device_index}, the current device is {torch.cuda.current_device()}")
-    return s.cuda_stream, s.device_index
+    device = torch.cuda.current_device()
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream, device
+    if stream.device_index != device:   # (kernels are launched on the current device)
+        raise ValueError(f"the stream belongs to device {stream.device_index}, the current device is {device}")
+    return stream.cuda_stream, device
 
 
 def make_cross_attn_desc(**kw) -> CrossAttnDesc:
@@ -360,22 +358,20 @@ def _cross_shapes(d):
 
 def slapo_cross_attn_fwd(desc, q, k, v, kv_lens, out, lse=None, ws=None, stream=None):
     """q, out [batch, q_len, heads * head_dim], k, v [batch, kv_len, kv_heads * head_dim], views with the descriptor's strides."""
-    need, _ = slapo_cross_attn_workspace(desc)
     st, dev = _stream_and_device(stream)
     dt, f32, (a, b, c, e) = _TORCH[desc.dtype], torch.float32, _cross_shapes(desc)
     _check(lib().slapo_cross_attn_fwd(C.byref(desc), _arg("q", q, dt, *a, dev), _arg("k", k, dt, *b, dev), _arg("v", v, dt, *b, dev),
                                       _arg("kv_lens", kv_lens, torch.int32, (desc.batch,), (1,), dev, True), _arg("out", out, dt, *c, dev),
-                                      _arg("lse", lse, f32, *e, dev, True), _room("ws", ws, need, dev), st), "slapo_cross_attn_fwd")
+                                      _arg("lse", lse, f32, *e, dev, True), *_room(ws, dev), st), "slapo_cross_attn_fwd")
 
 
 def slapo_cross_attn_bwd(desc, q, k, v, kv_lens, out, dout, lse, dq, dk, dv, ws, stream=None):
-    _, need = slapo_cross_attn_workspace(desc)
     st, dev = _stream_and_device(stream)
     dt, (a, b, c, e) = _TORCH[desc.dtype], _cross_shapes(desc)
     _check(lib().slapo_cross_attn_bwd(C.byref(desc), _arg("q", q, dt, *a, dev), _arg("k", k, dt, *b, dev), _arg("v", v, dt, *b, dev),
                                       _arg("kv_lens", kv_lens, torch.int32, (desc.batch,), (1,), dev, True), _arg("out", out, dt, *c, dev),
                                       _arg("dout", dout, dt, *c, dev), _arg("lse", lse, torch.float32, *e, dev), _arg("dq", dq, dt, *a, dev),
-                                      _arg("dk", dk, dt, *b, dev), _arg("dv", dv, dt, *b, dev), _room("ws", ws, need, dev), st),
+                                      _arg("dk", dk, dt, *b, dev), _arg("dv", dv, dt, *b, dev), *_room(ws, dev), st),
            "slapo_cross_attn_bwd")
 
 
@@ -400,7 +396,7 @@ def slapo_rope_axes(desc, positions, x, out, inverse=0, stream=None):
 def _rows(name, t, dtype, rows, width, stride, device):
     """Address of a tensor of `rows` rows of at least `width` elements, `stride` apart."""
     shape, strides = t.shape, t.stride()
-    ok = t.dtype is dtype and t.is_cuda and t.device.index == device and len(shape) >= 1 and shape[-1] >= width and strides[-1] == 1
+    ok = t.dtype is dtype and t.is_cuda and t.get_device() == device and len(shape) >= 1 and shape[-1] >= width and strides[-1] == 1
     n = 1
     for size, step in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         ok = ok and (size == 1 or step == n * stride)
@@ -424,7 +420,7 @@ class GradPlan:
         for i, (g, o) in enumerate(zip(grads, out)):
             for t in (g, o):
                 if t is not None and (t.dtype not in _DTYPE or t.dtype is not g.dtype or t.numel() != g.numel() or not t.is_contiguous()
-                                      or not t.is_cuda or t.device.index != self.device):
+                                      or not t.is_cuda or t.get_device() != self.device):
                     _refuse(f"gradient {i}", t, f"contiguous {g.dtype} of {g.numel()} elements")
             table[i] = _Grad(g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), _DTYPE[g.dtype])
         need = C.c_size_t(0)
@@ -437,7 +433,7 @@ class GradPlan:
 def _scalar(name, t, dtype, device, optional=False):
     if t is None and optional:
         return None
-    if t.dtype is not dtype or t.numel() != 1 or not t.is_cuda or t.device.index != device:
+    if t.dtype is not dtype or t.numel() != 1 or not t.is_cuda or t.get_device() != device:
         _refuse(name, t, f"one {dtype}")
     return t.data_ptr()
 

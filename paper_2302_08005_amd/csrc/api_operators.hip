@@ -158,13 +158,15 @@ int slapo_cross_attn_workspace(const slapo_cross_attn_desc* d, size_t* fwd_bytes
 }
 
 int slapo_cross_attn_fwd(const slapo_cross_attn_desc* d, const void* q, const void* k, const void* v, const int32_t* kv_lens, void* out,
-                         float* lse, void* ws, void* stream) {
+                         float* lse, void* ws, size_t ws_bytes, void* stream) {
   const int rc = check_cross(d);
   if (rc) return rc;
   if (!q || !k || !v || !out) return SLAPO_ERR_NULL;
   const CrossShape s = cross_shape(d);
-  if (!ws && cross_attn_fwd_ws_bytes(d->dtype, d->head_dim, s)) return SLAPO_ERR_NULL;
+  const size_t need = cross_attn_fwd_ws_bytes(d->dtype, d->head_dim, s);
+  if (!ws && need) return SLAPO_ERR_NULL;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(ws)) return SLAPO_ERR_ALIGN;
+  if (ws_bytes < need) return SLAPO_ERR_WORKSPACE;
   CrossOperands p = {};
   p.q = q; p.k = k; p.v = v; p.lens = kv_lens; p.o = out; p.lse = lse; p.ws = (float*)ws;
   entry_error();
@@ -173,13 +175,14 @@ int slapo_cross_attn_fwd(const slapo_cross_attn_desc* d, const void* q, const vo
 }
 
 int slapo_cross_attn_bwd(const slapo_cross_attn_desc* d, const void* q, const void* k, const void* v, const int32_t* kv_lens, const void* out,
-                         const void* dout, const float* lse, void* dq, void* dk, void* dv, void* ws, void* stream) {
+                         const void* dout, const float* lse, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
   const int rc = check_cross(d);
   if (rc) return rc;
   if (!q || !k || !v || !out || !dout || !lse || !dq || !dk || !dv || !ws) return SLAPO_ERR_NULL;
   for (const void* a : {q, k, v, out, dout, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)ws})
     if (misaligned(a)) return SLAPO_ERR_ALIGN;
   const CrossShape s = cross_shape(d);
+  if (ws_bytes < cross_attn_bwd_ws_bytes(d->dtype, d->head_dim, s)) return SLAPO_ERR_WORKSPACE;
   CrossOperands p = {};
   p.q = q; p.k = k; p.v = v; p.lens = kv_lens; p.out = out; p.dout = dout; p.lse = const_cast<float*>(lse); p.dq = dq; p.dk = dk; p.dv = dv; p.ws = (float*)ws;
   entry_error();

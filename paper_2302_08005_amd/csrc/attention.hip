@@ -471,7 +471,6 @@ __device__ __forceinline__ void attn_bwd_dkdv_block(const BlockId blk, const Att
   constexpr int NSTG = DKDV_STAGES<D>;
   constexpr bool ACC_A = (D == 128);    // dK/dV accumulators in AGPRs (see mfma16_agpr)
   constexpr bool PIPE = ACC_A && !DROP && !SHORT; // hand-pipelined sub-tiles for tiles without a mask boundary (see compute)
-  static_assert(!PIPE || (NS == 8 && NT == 4), "the pipelined rounds are written for D = 128");
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];
   const int S = sh.seq, H = sh.hidden;
   const int b = blk.b, a = blk.a, kv_base = blk.x * RB;
@@ -571,127 +570,10 @@ __device__ __forceinline__ void attn_bwd_dkdv_block(const BlockId blk, const Att
     const bf16_t* dtile = qtile + TE;
     const float* stats = reinterpret_cast<const float*>(qtile + 2 * TE);
     if constexpr (PIPE) {
-      // One wavefront per SIMD (128-wide heads): nothing else runs while this wavefront does the softmax
-      // arithmetic of a sub-tile, so for tiles without a mask boundary the two sub-tiles are software-
-      // pipelined by hand: every MFMA is followed by the vector work of one score element of the OTHER
-      // sub-tile, which issues while the matrix core is busy.
-      //   scores(0);  scores(1) || softmax(0);  dV,dK(0) || softmax(1);  dV,dK(1)
+      // (see dkdv_interior; interior: no mask boundary)
       const bool interior = !wave_kv_edge && q0 + 64 <= S && !(sh.causal && q0 < wave_kv_min + 32);
       if (interior) {
-        f32x16_t sc0, dp0, sc1, dp1;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc0[r] = dp0[r] = sc1[r] = dp1[r] = 0.f;
-        // scores of sub-tile 0
-#pragma unroll
-        for (int s0 = 0; s0 < NS; s0 += FB) {
-          bf16x8_t fq[FB], fd[FB];
-#pragma unroll
-          for (int s = 0; s < FB; ++s) {
-            fq[s] = frag_rows<D>(qtile, fr_base, 0, s0 + s);
-            fd[s] = frag_rows<D>(dtile, fr_base, 0, s0 + s);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int s = 0; s < FB; ++s) {
-            sc0 = mfma16<F16>(fq[s], kf[s0 + s], sc0);
-            dp0 = mfma16<F16>(fd[s], vf[s0 + s], dp0);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        // The 16 score elements of a sub-tile go through three steps each - a = sc * scale - lse; p = exp2(a);
-        // sc = p, dp = p * (dp - delta) - and run as a pipeline beside 16 MFMAs of the OTHER sub-tile: the slot of
-        // MFMA s holds step 1 of element s + 1, step 2 of element s and step 3 of element s - 1, so no vector
-        // instruction waits for the result of the one in front of it (one element's steps back to back are a
-        // dependent chain whose latencies nothing hides with a single wavefront per SIMD). The row statistics of
-        // four elements (one float4 each of lse and delta) are read from LDS three slots ahead of their first use.
-        auto pick = [](const float4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; };
-        auto soft_slots = [&](f32x16_t& sc, f32x16_t& dp, const float* srow, auto&& mfma_slot) {
-          float4 l[2], d[2];
-          l[0] = *reinterpret_cast<const float4*>(srow + 4 * kc);
-          d[0] = *reinterpret_cast<const float4*>(srow + 64 + 4 * kc);
-          float a_next = fmaf(sc[0], sl2, -l[0].x), p_prev = 0.f;
-#pragma unroll
-          for (int s = 0; s < 16; ++s) {
-            const int g = s >> 2, e = s & 3;
-            if (e == 1 && g + 1 < 4) {
-              l[(g + 1) & 1] = *reinterpret_cast<const float4*>(srow + (g + 1) * 8 + 4 * kc);
-              d[(g + 1) & 1] = *reinterpret_cast<const float4*>(srow + 64 + (g + 1) * 8 + 4 * kc);
-            }
-            mfma_slot(s);
-            const float a_cur = a_next;
-            if (s + 1 < 16) a_next = fmaf(sc[s + 1], sl2, -pick(l[((s + 1) >> 2) & 1], (s + 1) & 3));
-            const float p_cur = __builtin_amdgcn_exp2f(a_cur);
-            if (s > 0) {
-              sc[s - 1] = p_prev;
-              dp[s - 1] = p_prev * (dp[s - 1] - pick(d[((s - 1) >> 2) & 1], (s - 1) & 3));
-            }
-            p_prev = p_cur;
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          sc[15] = p_prev;
-          dp[15] = p_prev * (dp[15] - d[1].w);
-        };
-        // scores of sub-tile 1 (two k-steps = four MFMAs per round) || softmax of sub-tile 0
-        {
-          bf16x8_t fq[2][2], fd[2][2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) { fq[0][k] = frag_rows<D>(qtile, fr_base, 32, k); fd[0][k] = frag_rows<D>(dtile, fr_base, 32, k); }
-          soft_slots(sc0, dp0, stats, [&](int s) {
-            const int g = s >> 2, e = s & 3, cur = g & 1;
-            if (e == 0 && g + 1 < NS / 2) {
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                fq[cur ^ 1][k] = frag_rows<D>(qtile, fr_base, 32, 2 * g + 2 + k);
-                fd[cur ^ 1][k] = frag_rows<D>(dtile, fr_base, 32, 2 * g + 2 + k);
-              }
-            }
-            // (a compiler-visible MFMA is a pure operation that the instruction selector may move past scheduling
-            // barriers - all sixteen ended up behind the softmax; the empty statement pins its result to this slot)
-            if (e == 0) { sc1 = mfma16<F16>(fq[cur][0], kf[2 * g], sc1); pin_here(sc1); }
-            else if (e == 1) { dp1 = mfma16<F16>(fd[cur][0], vf[2 * g], dp1); pin_here(dp1); }
-            else if (e == 2) { sc1 = mfma16<F16>(fq[cur][1], kf[2 * g + 1], sc1); pin_here(sc1); }
-            else { dp1 = mfma16<F16>(fd[cur][1], vf[2 * g + 1], dp1); pin_here(dp1); }
-          });
-        }
-        // dV, dK of sub-tile 0 (four MFMAs per round) || softmax of sub-tile 1
-        {
-          const bf16x8_t pf[2] = {pack8<F16>(sc0, 0), pack8<F16>(sc0, 1)}, dsf[2] = {pack8<F16>(dp0, 0), pack8<F16>(dp0, 1)};
-          bf16x8_t td[2][2], tq[2][2];   // [round parity][column block of the round]
-#pragma unroll
-          for (int k = 0; k < 2; ++k) { td[0][k] = frag_tr<D>(dtile, ft_base, 0, k); tq[0][k] = frag_tr<D>(qtile, ft_base, 0, k); }
-          soft_slots(sc1, dp1, stats + 32, [&](int s) {   // round g: half h = g / 2, column blocks t = 2 (g % 2), 2 (g % 2) + 1
-            const int g = s >> 2, e = s & 3, cur = g & 1, h = g >> 1, t0 = 2 * (g & 1);
-            if (e == 0 && g + 1 < 4) {
-              const int hn = (g + 1) >> 1, tn = 2 * ((g + 1) & 1);
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                td[cur ^ 1][k] = frag_tr<D>(dtile, ft_base, 16 * hn, tn + k);
-                tq[cur ^ 1][k] = frag_tr<D>(qtile, ft_base, 16 * hn, tn + k);
-              }
-            }
-            if (e == 0) mfma16_agpr<F16>(dv[t0], td[cur][0], pf[h]);
-            else if (e == 1) mfma16_agpr<F16>(dk[t0], tq[cur][0], dsf[h]);
-            else if (e == 2) mfma16_agpr<F16>(dv[t0 + 1], td[cur][1], pf[h]);
-            else mfma16_agpr<F16>(dk[t0 + 1], tq[cur][1], dsf[h]);
-          });
-        }
-        // dV, dK of sub-tile 1
-        {
-          const bf16x8_t pf[2] = {pack8<F16>(sc1, 0), pack8<F16>(sc1, 1)}, dsf[2] = {pack8<F16>(dp1, 0), pack8<F16>(dp1, 1)};
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            bf16x8_t td[NT], tq[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              td[t] = frag_tr<D>(dtile, ft_base, 32 + 16 * h, t);
-              tq[t] = frag_tr<D>(qtile, ft_base, 32 + 16 * h, t);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) { mfma16_agpr<F16>(dv[t], td[t], pf[h]); mfma16_agpr<F16>(dk[t], tq[t], dsf[h]); }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
+        dkdv_interior<F16>(qtile, dtile, stats, kf, vf, dk, dv, fr_base, ft_base, kc, sl2);
         return;
       }
     }

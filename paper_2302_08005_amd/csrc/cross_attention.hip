@@ -44,18 +44,26 @@ __device__ __forceinline__ f32x4_t rows_times_rows(const RowFrags<D>& a, const R
 // row lane % 16 of w. x(row): element of this lane's column in that row; rows from n on (to the next multiple of 16) count as zeros.
 template <class X>
 __device__ __forceinline__ f32x4_t weighted_rows(f32x4_t acc, const float* w, int n, int g, X&& x) {
-  for (int t = 0; t < n; t += 16) {
-    const float4 wv = *reinterpret_cast<const float4*>(w + t + 4 * g);
-    float v[4];
+  constexpr int U = 4;   // tiles of 16 rows in flight: the walk is a chain of load latencies
+  for (int t0 = 0; t0 < n; t0 += 16 * U) {
+    float v[U][4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int row = t + 4 * g + s;
-      v[s] = row < n ? x(row) : 0.f;
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int row = t0 + 16 * u + 4 * g + s;
+        v[u][s] = x(min(row, n - 1));
+        v[u][s] = row < n ? v[u][s] : 0.f;
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + 16 * u >= n) break;   // (uniform)
+      const float4 wv = *reinterpret_cast<const float4*>(w + t0 + 16 * u + 4 * g);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][0], wv.x, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][1], wv.y, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][2], wv.z, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][3], wv.w, acc, 0, 0, 0);
     }
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[0], wv.x, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[1], wv.y, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[2], wv.z, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[3], wv.w, acc, 0, 0, 0);
   }
   return acc;
 }

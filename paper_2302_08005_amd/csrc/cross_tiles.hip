@@ -16,17 +16,22 @@ namespace slapo {
 
 namespace {
 
-struct CrossBlock { int x, head, split; };   // head: of all samples' key heads
+// head: of all samples' key heads, sample after sample
+struct CrossBlock { int x, b, h, head, split; };
 // Blocks are handed to the 8 XCDs round-robin in launch order; those of one head are renumbered to sit on one XCD next to each other in time, and
-// share the tiles through its L2.
-__device__ __forceinline__ CrossBlock cross_block(unsigned w, unsigned total, int nx, int splits) {
+// share the tiles through its L2. Neighbours of a head are heads of other samples, each key head's list beginning with another sample: samples differ in
+// length, and an XCD or a CU that had all heads of one would be done early or late.
+__device__ __forceinline__ CrossBlock cross_block(unsigned w, unsigned total, int nx, int splits, const CrossShape& sh) {
   const unsigned xcd = w & 7, q = total >> 3, r = total & 7;
   w = xcd * q + (xcd < r ? xcd : r) + (w >> 3);
   CrossBlock id;
   id.x = w % nx;
   w /= nx;
   id.split = w % splits;
-  id.head = w / splits;
+  w /= splits;
+  id.h = w / sh.batch;
+  id.b = (w + id.h) % sh.batch;
+  id.head = id.b * sh.kv_heads + id.h;
   return id;
 }
 // tiles of a split: the walk cut evenly
@@ -149,25 +154,26 @@ __device__ __forceinline__ void zero(f32x16_t (&v)[N]) {
     for (int r = 0; r < 16; ++r) v[t][r] = 0.f;
 }
 
-// Running softmax of a row (a lane holds half of it) and the output accumulated under it.
+// Running softmax of a row (a lane holds half of it) and the output accumulated under it. Probabilities are taken against m, which follows the
+// row's maximum from below: it moves when the maximum has grown by more than 2^GROWN since (and all that was accumulated is then scaled down), not
+// with every tile whose maximum is a little larger (of 32 rows, one has such a tile nearly always). They are at most 2^GROWN, which every type holds.
 template <int D>
 struct Softmax {
-  static constexpr int NT = D / 32;
+  static constexpr int NT = D / 32, GROWN = 8;
   f32x16_t o[NT];
-  float m = -INFINITY, l = 0.f;   // maximum (raw scores), sum of this lane's half
+  float m = -INFINITY, l = 0.f;   // what probabilities are relative to (raw scores), sum of this lane's half
   __device__ __forceinline__ Softmax() { zero(o); }
-  // 32-row sub-tiles of scores -> probabilities against the new maximum; the rest is scaled down where it grew
+  // 32-row sub-tiles of scores -> probabilities
   template <int SUBS>
-  __device__ __forceinline__ void add(f32x16_t (&sc)[SUBS], float sl2) {
+  __device__ __forceinline__ void add(f32x16_t (&sc)[SUBS], float sl2, float grown) {   // grown: GROWN / sl2
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < SUBS; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[i][r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float m_new = fmaxf(m, mx);
-    if (__any(m_new > m)) {
-      const float al = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * sl2);
+    if (__any(mx > m + grown)) {
+      const float m_new = fmaxf(m, mx), al = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * sl2);
       l *= al;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -218,8 +224,8 @@ template <int D, bool F16, int G>
 __global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOperands p, int nx, FwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // [2][G][K tile | V tile]
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits);
-  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits, sh);
+  const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
@@ -228,7 +234,7 @@ __global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOper
   const int first = split_begin(all_tiles, blk.split, parts.splits), n_tiles = split_begin(all_tiles, blk.split + 1, parts.splits) - first;
   const int wave_row = blk.x * RB + 32 * row_wave, my_row = wave_row + (lane & 31);
   const int64_t head0 = (int64_t)h * sh.group * D;
-  const float sl2 = LOG2E * sh.scale;
+  const float sl2 = LOG2E * sh.scale, grown = Softmax<D>::GROWN / sl2;
 
   const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
   bf16x8_t qf[NS];
@@ -264,7 +270,7 @@ __global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOper
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[i][r] = kv0 + i * 32 + acc_row(r, lane) >= n_keys ? -INFINITY : sc[i][r];
     }
-    sm.add(sc, sl2);
+    sm.add(sc, sl2, grown);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -311,31 +317,25 @@ __global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOper
 
 // ================================ forward: at most 32 rows of a head ====================================
 // A token or a few that are being generated: one wavefront has all rows, and the walk over the states is all there is to share. Bound by
-// reading them, so every wavefront walks tiles of 32 states of its own, NSTG of them on their way, and waits for nobody; its four
-// wavefronts' results meet in LDS, those of several blocks in a second kernel.
-template <int D> constexpr int FEW_STAGES = D == 64 ? 4 : 2;
+// reading them, so every wavefront walks tiles of 32 states of its own and waits for nobody: while one computes, the others' tiles are on
+// their way. Their results meet in LDS, those of several blocks in a second kernel.
+template <int D> constexpr int FEW_WAVES = D == 64 ? 16 : 8;   // (K and V tiles of all of them: 128 KB of LDS)
 template <int D, bool F16>
-__global__ __launch_bounds__(256) void cross_few_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
-  constexpr int NS = D / 16, NT = D / 32, TE = 32 * D, NSTG = FEW_STAGES<D>, SPR = D / 8, LOADS = SPR / 2;   // wave-level loads per tile of 32 rows
-  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // per wavefront [NSTG][K tile | V tile]
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, 1, parts.splits);
-  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+__global__ __launch_bounds__(64 * FEW_WAVES<D>) void cross_few_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, TE = 32 * D, WAVES = FEW_WAVES<D>, SPR = D / 8, LOADS = SPR / 2;   // LOADS: wave-level, of 32 rows
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // per wavefront [K tile | V tile]
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, 1, parts.splits, sh);
+  const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
   const CrossRows rows(sh);
   const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), all_tiles = (n_keys + 31) / 32;
   const int first = split_begin(all_tiles, blk.split, parts.splits) + wave, end = split_begin(all_tiles, blk.split + 1, parts.splits);
-  const int n_tiles = first < end ? (end - first + 3) / 4 : 0;   // this wavefront's: every fourth
   const int my_row = lane & 31;
   const int64_t head0 = (int64_t)h * sh.group * D;
-  const float sl2 = LOG2E * sh.scale;
-  const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
-  bf16x8_t qf[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(q + 16 * s + 8 * kc);
-  Softmax<D> sm;
+  const float sl2 = LOG2E * sh.scale, grown = Softmax<D>::GROWN / sl2;
 
-  bf16_t* mine = smem + wave * NSTG * 2 * TE;
+  bf16_t *ktile = smem + wave * 2 * TE, *vtile = ktile + TE;
   const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   const bf16_t *k = (const bf16_t*)p.k + kv0, *v = (const bf16_t*)p.v + kv0;
   const unsigned bytes = n_keys > 0 ? (unsigned)(((int64_t)(n_keys - 1) * sh.kv_stride + D) * 2) : 0u, step = (unsigned)(32 * sh.kv_stride * 2);
@@ -345,128 +345,115 @@ __global__ __launch_bounds__(256) void cross_few_kernel(CrossShape sh, CrossOper
     const int slot = i * 64 + lane, row = slot / SPR, pos = slot % SPR;
     voff[i] = (unsigned)(row * sh.kv_stride * 2) + (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
   }
-  auto issue = [&](int stage, int i) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wavefront has read of the stage has arrived
-    const unsigned at = (unsigned)(first + 4 * i) * step;
+  auto issue = [&](int t) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wavefront has read of the tile in front has arrived
+    const unsigned at = (unsigned)t * step;
 #pragma unroll
-    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(k, bytes, mine + stage * 2 * TE + n * 512, voff[n] + at, 0);
+    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(k, bytes, ktile + n * 512, voff[n] + at, 0);
 #pragma unroll
-    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(v, bytes, mine + stage * 2 * TE + TE + n * 512, voff[n] + at, 0);
+    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(v, bytes, vtile + n * 512, voff[n] + at, 0);
   };
-  auto compute = [&](int stage, int i) {
-    const int key0 = (first + 4 * i) * 32;
-    const bf16_t *ktile = mine + stage * 2 * TE, *vtile = ktile + TE;
+  if (first < end) issue(first);
+  const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
+  bf16x8_t qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(q + 16 * s + 8 * kc);
+  Softmax<D> sm;
+  for (int t = first; t < end; t += WAVES) {
+    wait_loads_and_lds<0>();
+    asm volatile("" ::: "memory");
     f32x16_t sc[1];
     zero(sc);
 #pragma unroll
     for (int s = 0; s < NS; ++s) sc[0] = mfma16<F16>(frag_rows<D>(ktile, fr_base, 0, s), qf[s], sc[0]);
-    if (key0 + 32 > n_keys) {
+    if (32 * t + 32 > n_keys) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[0][r] = key0 + acc_row(r, lane) >= n_keys ? -INFINITY : sc[0][r];
+      for (int r = 0; r < 16; ++r) sc[0][r] = 32 * t + acc_row(r, lane) >= n_keys ? -INFINITY : sc[0][r];
     }
-    sm.add(sc, sl2);
+    sm.add(sc, sl2, grown);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const bf16x8_t pf = pack8<F16>(sc[0], half);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) sm.o[t] = mfma16<F16>(frag_tr<D>(vtile, ft_base, 16 * half, t), pf, sm.o[t]);
+      for (int c = 0; c < NT; ++c) sm.o[c] = mfma16<F16>(frag_tr<D>(vtile, ft_base, 16 * half, c), pf, sm.o[c]);
     }
-  };
-  // the tile that is computed next has landed when at most the younger ones' loads are outstanding
-  auto wait_for_oldest = [&](int younger) {
-    if (younger >= 3 && NSTG > 3) wait_loads_and_lds<(NSTG > 3 ? 3 : 0) * 2 * LOADS>();
-    else if (younger == 2 && NSTG > 2) wait_loads_and_lds<(NSTG > 2 ? 2 : 0) * 2 * LOADS>();
-    else if (younger == 1) wait_loads_and_lds<2 * LOADS>();
-    else wait_loads_and_lds<0>();
-    asm volatile("" ::: "memory");
-  };
-#pragma unroll
-  for (int i = 0; i < NSTG - 1; ++i)
-    if (i < n_tiles) issue(i, i);
-  for (int i0 = 0; i0 < n_tiles; i0 += NSTG) {
-#pragma unroll
-    for (int s = 0; s < NSTG; ++s) {
-      const int i = i0 + s;
-      if (i >= n_tiles) break;   // uniform
-      if (i + NSTG - 1 < n_tiles) issue((s + NSTG - 1) % NSTG, i + NSTG - 1);   // (that stage's reads have been used)
-      wait_for_oldest(min(NSTG - 1, n_tiles - 1 - i));
-      compute(s, i);
-    }
+    if (t + WAVES < end) issue(t + WAVES);
   }
-  // wavefront w puts together columns 32 w .. of all four
+  // every wavefront puts some of the accumulators of all together: registers REGS w .. of the 16 NT
   __syncthreads();
-  constexpr int REGS = NT * 16 + 2;
-  float* slots = reinterpret_cast<float*>(smem);
+  constexpr int REGS = 16 * NT / WAVES, SLOT = 16 * NT + 2;
+  static_assert(REGS % 2 == 0 && 16 % REGS == 0, "whole pairs of columns, of one 32-column block");
+  float* slots = reinterpret_cast<float*>(smem) + lane;
   {
-    float* s = slots + wave * REGS * 64 + lane;
+    float* s = slots + wave * SLOT * 64;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[(t * 16 + r) * 64] = sm.o[t][r];
-    s[NT * 16 * 64] = sm.m;
-    s[(NT * 16 + 1) * 64] = sm.l + __shfl_xor(sm.l, 32, 64);
+    s[16 * NT * 64] = sm.m;
+    s[(16 * NT + 1) * 64] = sm.l + __shfl_xor(sm.l, 32, 64);
   }
   __syncthreads();
-  if (wave >= NT) return;
-  float m = -INFINITY, l = 0.f, weight[4];
-#pragma unroll
-  for (int w = 0; w < 4; ++w) m = fmaxf(m, slots[(w * REGS + NT * 16) * 64 + lane]);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    weight[w] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((slots[(w * REGS + NT * 16) * 64 + lane] - m) * sl2);
-    l += weight[w] * slots[(w * REGS + NT * 16 + 1) * 64 + lane];
-  }
-  const float inv = inverse(l);
   if (my_row >= n_rows) return;
-  float o[16];
+  float m = -INFINITY, l = 0.f, o[REGS];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    o[r] = 0.f;
+  for (int w = 0; w < WAVES; ++w) m = fmaxf(m, slots[(w * SLOT + 16 * NT) * 64]);
+  const float base = m == -INFINITY ? 0.f : m * sl2;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) o[r] += weight[w] * slots[(w * REGS + wave * 16 + r) * 64 + lane];
-    o[r] *= inv;
+  for (int r = 0; r < REGS; ++r) o[r] = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const float weight = __builtin_amdgcn_exp2f(fmaf(slots[(w * SLOT + 16 * NT) * 64], sl2, -base));
+    l = fmaf(weight, slots[(w * SLOT + 16 * NT + 1) * 64], l);
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) o[r] = fmaf(weight, slots[(w * SLOT + wave * REGS + r) * 64], o[r]);
   }
-  const float my_lse = log_sum(m, l, sh.scale);
-  const int col = wave * 32 + 4 * kc;
-  if (parts.splits > 1) {
-    float* dst = parts.rows<D>(blk.head, blk.split, n_rows, my_row) + col;
+  const float inv = inverse(l), my_lse = log_sum(m, l, sh.scale);
+  const int reg = wave * REGS % 16, col = wave * REGS / 16 * 32 + 8 * (reg / 4) + 4 * kc + reg % 4;   // of o[0]
+  bf16_t* out = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(my_row, sh.out_stride, D) + col;
+  float* part = parts.splits > 1 ? parts.rows<D>(blk.head, blk.split, n_rows, my_row) + col : nullptr;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(dst + 8 * g) = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
-    if (wave == 0 && kc == 0) *parts.stat(blk.head, blk.split, n_rows, my_row) = my_lse;
-  } else {
-    bf16_t* dst = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0 + rows.at(my_row, sh.out_stride, D) + col;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) *reinterpret_cast<uint2*>(dst + 8 * g) = make_uint2(pack2<F16>(o[4 * g], o[4 * g + 1]), pack2<F16>(o[4 * g + 2], o[4 * g + 3]));
-    if (p.lse && wave == 0 && kc == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(my_row)] = my_lse;
+  for (int r = 0; r < REGS; r += 2) {   // (registers 4 g .. 4 g + 3: consecutive columns; the next four eight columns on)
+    const int c = r / 4 * 8 + r % 4;
+    if (part) *reinterpret_cast<float2*>(part + c) = make_float2(o[r] * inv, o[r + 1] * inv);
+    else *reinterpret_cast<uint32_t*>(out + c) = pack2<F16>(o[r] * inv, o[r + 1] * inv);
+  }
+  if (wave == 0 && kc == 0) {
+    if (part) *parts.stat(blk.head, blk.split, n_rows, my_row) = my_lse;
+    else if (p.lse) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(my_row)] = my_lse;
   }
 }
 
-// Puts the splits of a row together, by their logsumexps: a wavefront per row.
+// Puts the splits of a row together, by their logsumexps: eight columns per thread.
 constexpr int MAX_SPLITS = 64;
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
+  constexpr int C = D / 8;
   const CrossRows rows(sh);
-  const int n_rows = rows.count(), lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= (int64_t)sh.batch * sh.kv_heads * n_rows) return;
-  const int head = (int)(item / n_rows), r = (int)(item - (int64_t)head * n_rows), b = head / sh.kv_heads, h = head - b * sh.kv_heads;
-  const float lse = lane < parts.splits ? *parts.stat(head, lane, n_rows, r) : -INFINITY;
-  const float m = wave_max(lse), base = m == -INFINITY ? 0.f : m;
-  const float e = __expf(lse - base), total = wave_sum(e), weight = e * inverse(total);
-  constexpr int C = D / 64;
-  float o[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) o[c] = 0.f;
+  const int n_rows = rows.count();
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / C;
+  if (row >= (int64_t)sh.batch * sh.kv_heads * n_rows) return;
+  const int head = (int)(row / n_rows), r = (int)(row - (int64_t)head * n_rows), b = head / sh.kv_heads, h = head - b * sh.kv_heads, c = 8 * (int)(i % C);
+  const float* lse = parts.stat(head, 0, n_rows, r);
+  const float* src = parts.rows<D>(head, 0, n_rows, r) + c;
+  float m = -INFINITY;
+  for (int s = 0; s < parts.splits; ++s) m = fmaxf(m, lse[(int64_t)s * n_rows]);
+  const float base = m == -INFINITY ? 0.f : m;
+  float total = 0.f, o[8] = {};
+#pragma unroll 4
   for (int s = 0; s < parts.splits; ++s) {
-    const float w = __shfl(weight, s, 64);
-    const float* src = parts.rows<D>(head, s, n_rows, r) + C * lane;
+    const float weight = __expf(lse[(int64_t)s * n_rows] - base);
+    float v[8];
+    load8(src + (int64_t)s * n_rows * D, v);
+    total += weight;
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = fmaf(w, src[c], o[c]);
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(weight, v[e], o[e]);
   }
-  bf16_t* dst = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + (int64_t)h * sh.group * D + rows.at(r, sh.out_stride, D) + C * lane;
-  if constexpr (C == 2) *reinterpret_cast<uint32_t*>(dst) = pack2<F16>(o[0], o[1]);
-  else *dst = (bf16_t)(pack2<F16>(o[0], 0.f) & 0xffffu);
-  if (p.lse && lane == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(r)] = total != 0.f ? base + __logf(total) : -INFINITY;
+  const float inv = inverse(total);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] *= inv;
+  store8h<F16>((bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + (int64_t)h * sh.group * D + rows.at(r, sh.out_stride, D) + c, o);
+  if (p.lse && c == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(r)] = total != 0.f ? base + __logf(total) : -INFINITY;
 }
 
 // ======================================== backward ======================================================
@@ -482,11 +469,11 @@ struct BwdParts {
 
 // dQ of 128 / G rows. Also leaves delta = rowsum(dO * O) of its rows, laid out as lse, for the kernel of dK and dV.
 template <int D, bool F16, int G>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 1) void cross_dq_kernel(CrossShape sh, CrossOperands p, int nx, float* __restrict__ delta, BwdParts parts) {
+__global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kernel(CrossShape sh, CrossOperands p, int nx, float* __restrict__ delta, BwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // [2][G][K tile | V tile]
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits);
-  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits, sh);
+  const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
@@ -626,8 +613,8 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
   constexpr int FB = 4;                 // k-steps of fragment prefetch
   constexpr bool ACC_A = D == 128;      // dK/dV accumulators in AGPRs (see mfma16_agpr)
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits);
-  const int b = blk.head / sh.kv_heads, h = blk.head - b * sh.kv_heads;
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits, sh);
+  const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
@@ -676,6 +663,12 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
     const bf16_t* qtile = smem + stage * STAGE + grp * TILE;
     const bf16_t* dtile = qtile + TE;
     const float* stat = reinterpret_cast<const float*>(qtile + 2 * TE);
+    if constexpr (D == 128 && G == 1) {   // (two groups' tiles leave no registers for it)
+      if (!key_edge && q0 + 64 <= n_rows) {   // no mask boundary
+        dkdv_interior<F16>(qtile, dtile, stat, kf, vf, dk, dv, fr_base, ft_base, kc, sl2);
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int qs = q0 + i * 32;
@@ -850,11 +843,21 @@ Form form(int64_t rows, int64_t walk, int64_t heads) {
   return f;
 }
 constexpr int FEW_ROWS = 32;
-int few_splits(int64_t walk, int64_t heads) {
-  const int64_t tiles = (walk + 31) / 32;
-  int splits = 1;
-  while (splits < MAX_SPLITS && heads * splits * 2 <= 512 && tiles >= 8 * 2 * splits) splits *= 2;
-  return splits;
+// Blocks that share a walk over the states. Estimated in us, for what a block at a time on each CU takes: 3 for a block's beginning and end, for
+// every step of its wavefronts over tiles (128 KB) what a CU's rate of reading (37 GB/s) or the memory's (5.9 TB/s) takes, 4 for the second kernel.
+// Measured for 1 / 2 / 4 / 8: 16 samples x 16384 states, 8 key heads of 128 242 / 182 / 187 / 198 (estimate 227 / 189 / 193 / 198); 8 x 1024, 16 of 64
+// 11.0 / 12.9 / 16.4.
+int few_splits(int head_dim, int64_t walk, int64_t heads) {
+  const int64_t tiles = (walk + 31) / 32, waves = head_dim == 64 ? 16 : 8;
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= MAX_SPLITS && (s == 1 || tiles >= waves * s); ++s) {
+    const int64_t blocks = heads * s, rounds = (blocks + 255) / 256, steps = (tiles + waves * s - 1) / (waves * s);
+    const double step = std::max(131072 / 37e3, (blocks < 256 ? blocks : 256) * (131072 / 5.9e6));
+    const double t = rounds * (3.0 + steps * step) + (s > 1 ? 4.0 : 0.0);
+    if (t < least) { least = t; best = s; }
+  }
+  return best;
 }
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -863,7 +866,7 @@ FwdPlan fwd_plan(int head_dim, const CrossShape& s) {
   FwdPlan f;
   const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
   f.few = rows <= FEW_ROWS;
-  f.form = f.few ? Form{4, 1, few_splits(s.kv_len, heads)} : form(rows, s.kv_len, heads);
+  f.form = f.few ? Form{1, 1, few_splits(head_dim, s.kv_len, heads)} : form(rows, s.kv_len, heads);
   const size_t all = (size_t)(heads * rows * f.form.splits);
   f.o_bytes = f.form.splits > 1 ? up256(all * head_dim * 4) : 0;
   f.total = f.form.splits > 1 ? f.o_bytes + up256(all * 4) : 0;
@@ -882,10 +885,10 @@ BwdPlan bwd_plan(int head_dim, const CrossShape& s) {
   return f;
 }
 
-template <class Kernel, class... Args>
+template <int THREADS = 256, class Kernel, class... Args>
 void launch(Kernel kernel, int64_t blocks, size_t lds, hipStream_t st, Args... args) {
   if (lds > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, st, args...);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(THREADS), lds, st, args...);
 }
 
 template <int D, bool F16>
@@ -895,10 +898,10 @@ void fwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   const FwdParts parts = {p.ws, (float*)((char*)p.ws + f.o_bytes), f.form.splits};
   constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t);   // K and V
   const int64_t blocks = heads * f.form.nx * f.form.splits;
-  if (f.few) launch(cross_few_kernel<D, F16>, blocks, FEW_STAGES<D> * 4 * tile / 2, st, s, p, parts);
+  if (f.few) launch<64 * FEW_WAVES<D>>(cross_few_kernel<D, F16>, blocks, std::max(FEW_WAVES<D> * tile / 2, (size_t)FEW_WAVES<D> * (D / 2 + 2) * 64 * sizeof(float)), st, s, p, parts);
   else if (f.form.groups == 2) launch(cross_fwd_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.form.nx, parts);
   else launch(cross_fwd_kernel<D, F16, 1>, blocks, std::max(2 * tile, (size_t)4 * RowStage<D, F16>::ELEMS * 2), st, s, p, f.form.nx, parts);
-  if (f.form.splits > 1) launch(cross_join_kernel<D, F16>, (heads * rows + 3) / 4, 0, st, s, p, parts);
+  if (f.form.splits > 1) launch(cross_join_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts);
 }
 
 template <int D, bool F16>

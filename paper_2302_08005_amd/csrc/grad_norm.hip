@@ -25,22 +25,36 @@ __global__ __launch_bounds__(256) void grad_plan_kernel(GradTable table, int fir
   for (int64_t i = threadIdx.x; i < n && e.first + i < segments; i += 256) map[e.first + i] = first_entry + blockIdx.x;
 }
 
+constexpr int IN_FLIGHT = 4;   // loads of eight elements that a thread has on their way
+
 // elements [from, to) of a segment's array, `from` a multiple of 8
 template <typename T>
 __device__ __forceinline__ double sum_squares(const T* x, int64_t from, int64_t to) {
-  double s = 0.0;
-  int64_t i = from + 8 * (int64_t)threadIdx.x;
-  for (; i + 8 <= to; i += 8 * 256) {
+  double s[IN_FLIGHT] = {};
+  const auto add = [](double& s, const Raw8<T>& r) {
     float v[8];
-    load8(x + i, v);
+    r.get(v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
+  };
+  int64_t i = from + 8 * (int64_t)threadIdx.x;
+  for (; i + 8 * 256 * (IN_FLIGHT - 1) + 8 <= to; i += 8 * 256 * IN_FLIGHT) {
+    Raw8<T> r[IN_FLIGHT];
+#pragma unroll
+    for (int u = 0; u < IN_FLIGHT; ++u) r[u].load(x + i + 8 * 256 * u);
+#pragma unroll
+    for (int u = 0; u < IN_FLIGHT; ++u) add(s[u], r[u]);
+  }
+  for (; i + 8 <= to; i += 8 * 256) {
+    Raw8<T> r;
+    r.load(x + i);
+    add(s[0], r);
   }
   for (; i < to; ++i) {   // (only the last thread's)
     const double v = (double)to_f32(x[i]);
-    s = fma(v, v, s);
+    s[0] = fma(v, v, s[0]);
   }
-  return s;
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 // Sum over the block, in thread 0.
@@ -69,10 +83,11 @@ __global__ __launch_bounds__(256) void grad_sumsq_kernel(int64_t segments, int64
   }
   s = block_sum(s, shared);
   if (threadIdx.x == 0) {
+    // Sums and counter are device-wide atomics, which go past the caches that blocks on other dies do not share, so order between the two is all
+    // that is wanted, and no cache is written back.
     __hip_atomic_store(partials + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the sum is there
     last = atomicInc(counter, gridDim.x - 1) == gridDim.x - 1;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   }
   __syncthreads();
   if (!last) return;
@@ -84,13 +99,25 @@ __global__ __launch_bounds__(256) void grad_sumsq_kernel(int64_t segments, int64
 
 template <typename T>
 __device__ __forceinline__ void scale_segment(const T* in, T* out, int64_t from, int64_t to, float factor, float step) {
-  int64_t i = from + 8 * (int64_t)threadIdx.x;
-  for (; i + 8 <= to; i += 8 * 256) {
+  const auto put = [&](int64_t i, const Raw8<T>& r) {
     float v[8];
-    load8(in + i, v);
+    r.get(v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = v[k] * step * factor;
     store8(out + i, v);
+  };
+  int64_t i = from + 8 * (int64_t)threadIdx.x;
+  for (; i + 8 * 256 * (IN_FLIGHT - 1) + 8 <= to; i += 8 * 256 * IN_FLIGHT) {
+    Raw8<T> r[IN_FLIGHT];
+#pragma unroll
+    for (int u = 0; u < IN_FLIGHT; ++u) r[u].load(in + i + 8 * 256 * u);
+#pragma unroll
+    for (int u = 0; u < IN_FLIGHT; ++u) put(i + 8 * 256 * u, r[u]);
+  }
+  for (; i + 8 <= to; i += 8 * 256) {
+    Raw8<T> r;
+    r.load(in + i);
+    put(i, r);
   }
   for (; i < to; ++i) from_f32(out[i], to_f32(in[i]) * step * factor);
 }

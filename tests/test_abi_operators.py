@@ -29,17 +29,26 @@ def test_cross_attention_pointers():
     L, d = B.lib(), C.byref(cross())
     assert L.slapo_cross_attn_workspace(d, None, None) == -1 and L.slapo_cross_attn_workspace(None, C.byref(C.c_size_t()), C.byref(C.c_size_t())) == -1
     for i in (0, 1, 2, 4):
-        args = [P, P, P, None, P, None, P, None]
+        args = [P, P, P, None, P, None, P, 1 << 30, None]
         args[i] = None
         assert L.slapo_cross_attn_fwd(d, *args) == -1, i
         args[i] = P + 8
         assert L.slapo_cross_attn_fwd(d, *args) == -4, i
     for i in (0, 1, 2, 4, 5, 7, 8, 9, 10):
-        args = [P, P, P, None, P, P, P, P, P, P, P, None]
+        args = [P, P, P, None, P, P, P, P, P, P, P, 1 << 30, None]
         args[i] = None
         assert L.slapo_cross_attn_bwd(d, *args) == -1, i
         args[i] = P + 8
         assert L.slapo_cross_attn_bwd(d, *args) == -4, i
+
+
+def test_workspaces_that_are_too_small():
+    L, d = B.lib(), cross(batch=1, q_len=1, kv_len=4096)   # (few blocks: the walk is split)
+    fwd, bwd = B.slapo_cross_attn_workspace(d)
+    assert fwd > 0 and bwd > 0
+    assert L.slapo_cross_attn_fwd(C.byref(d), P, P, P, None, P, None, P, fwd - 1, None) == -5
+    assert L.slapo_cross_attn_fwd(C.byref(d), P, P, P, None, P, None, None, fwd, None) == -1
+    assert L.slapo_cross_attn_bwd(C.byref(d), P, P, P, None, P, P, P, P, P, P, P, bwd - 1, None) == -5
 
 
 def test_division_by_the_group_is_exact():
@@ -103,9 +112,7 @@ def test_host_tensors_are_refused():
     with pytest.raises(ValueError):
         B._arg("q", t, torch.float32, (2, 8, 256), t.stride(), 0)
     with pytest.raises(ValueError):
-        B._room("ws", t, 16, 0)
-    with pytest.raises(ValueError):
-        B._room("ws", None, 16, 0)
+        B._room(t, 0)
     with pytest.raises(ValueError):
         B._rows("x", t, torch.float32, 16, 256, 256, 0)
-    assert B._room("ws", None, 0, 0) is None
+    assert B._room(None, 0) == (None, 0)

@@ -177,10 +177,12 @@ def test_refused_tensors():
         with pytest.raises(ValueError):
             B.slapo_cross_attn_fwd(p.desc, **{**ok, **kw})
     p.forward()
+    for ws, status in ((p.ws[1][:16], -5), (None, -1)):
+        with pytest.raises(B.SlapoError) as e:
+            B.slapo_cross_attn_bwd(p.desc, p.q, p.k, p.v, None, p.out, p.do, p.lse, p.dq, p.dk, p.dv, ws)
+        assert e.value.status == status
     with pytest.raises(ValueError):
-        B.slapo_cross_attn_bwd(p.desc, p.q, p.k, p.v, None, p.out, p.do, p.lse, p.dq, p.dk, p.dv, p.ws[1][:-4])
-    with pytest.raises(ValueError):
-        B.slapo_cross_attn_bwd(p.desc, p.q, p.k, p.v, None, p.out, p.do, p.lse, p.dq, p.dk, p.dv, None)
+        B.slapo_cross_attn_bwd(p.desc, p.q, p.k, p.v, None, p.out, p.do, p.lse, p.dq, p.dk, p.dv, p.ws[1].cpu())
 
 
 def test_on_another_stream_and_replayed():
