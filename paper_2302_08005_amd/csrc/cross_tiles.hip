@@ -112,6 +112,33 @@ struct RowStage {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
+  // the same in the room of 16 rows
+  template <class Value, class Address>
+  static __device__ __forceinline__ void store_halves(bf16_t* stage, int lane, int rows, Value&& value, Address&& address) {
+    const int row = lane & 31, col = 4 * (lane >> 5);
+    constexpr int CPR = D / 8, RPI = 64 / CPR;
+    const int c = (lane % CPR) * 8;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      meet();
+      if (row >> 4 == half) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<uint2*>(stage + (row & 15) * P + t * 32 + g * 8 + col) =
+                make_uint2(pack2<F16>(value(t, 4 * g), value(t, 4 * g + 1)), pack2<F16>(value(t, 4 * g + 2), value(t, 4 * g + 3)));
+      }
+      meet();
+#pragma unroll
+      for (int k = 0; k < 16 / RPI; ++k) {
+        const int r = k * RPI + lane / CPR;
+        const uint2* p = reinterpret_cast<const uint2*>(stage + r * P + c);
+        const uint2 w0 = p[0], w1 = p[1];
+        if (16 * half + r < rows) *reinterpret_cast<uint4*>(address(16 * half + r) + c) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+      }
+    }
+  }
   template <class Value, class Address>
   static __device__ __forceinline__ void store(bf16_t* stage, int lane, int rows, Value&& value, Address&& address) {
     const int row = lane & 31, col = 4 * (lane >> 5);
@@ -804,6 +831,280 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
   RowStage<D, F16>::store(stage, lane, min(32, there), dv_value, [&](int r) { return (bf16_t*)p.dv + at + r * sh.kv_stride; });
 }
 
+// ===================================== at most 128 states ===============================================
+// A prompt, the latents of a resampler, the patches of a small image: all states of a head fit into LDS and every wavefront sees all of them, so a
+// wavefront needs nobody else: it takes tiles of 32 rows of its own, one after the other, the next one on its way, and softmax and delta are those
+// of whole rows. (Tiles shared by the wavefronts of a block, with barriers between their steps, took 1.5 times as long for backward.)
+constexpr int SHORT_KEYS = 128;
+// 32-row tiles of an operand whose rows are CrossRows, for one wavefront.
+template <int D>
+struct RowTiles {
+  static constexpr int SPR = D / 8, LOADS = SPR / 2;
+  unsigned bytes;
+  const bf16_t* base;
+  const CrossRows& rows;
+  int64_t stride;
+  int lane;
+  __device__ __forceinline__ RowTiles(const CrossRows& rows, const bf16_t* base, int64_t stride, int lane) : base(base), rows(rows), stride(stride), lane(lane) {
+    bytes = (unsigned)(((int64_t)(rows.q_len - 1) * stride + rows.group * D) * 2);
+  }
+  __device__ __forceinline__ void issue(bf16_t* tile, int row0) const {
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+      const int slot = k * 64 + lane, row = slot / SPR, pos = slot % SPR, t = rows.token(row0 + row);
+      const unsigned at = (unsigned)((t * (int)stride + (row0 + row - t * rows.group) * D) * 2) + (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
+      buffer_load_lds_16_untracked(base, bytes, tile + k * 512, at, 0);
+    }
+  }
+};
+// K and V of all visible states of a head, zeros behind them, as one or two 64-row tiles each.
+template <int D, int KEYS>
+__device__ __forceinline__ void load_states(const CrossShape& sh, const CrossOperands& p, int64_t kv0, int n_keys, bf16_t* ktile, bf16_t* vtile, int lane, int wave) {
+  const StateTiles<D> kt((const bf16_t*)p.k + kv0, sh.kv_stride, n_keys, lane, wave), vt((const bf16_t*)p.v + kv0, sh.kv_stride, n_keys, lane, wave);
+  kt.issue(ktile, 0);
+  vt.issue(vtile, 0);
+  if (KEYS == 128) {
+    kt.issue(ktile + Tile<D>::ELEMS, 1);   // (out of bounds where there are at most 64: zeros)
+    vt.issue(vtile + Tile<D>::ELEMS, 1);
+  }
+}
+
+template <int D> constexpr size_t SHORT_FWD_LDS = (4 * Tile<D>::ELEMS + 4 * 2 * 32 * D) * sizeof(bf16_t);
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void cross_fwd_short_kernel(CrossShape sh, CrossOperands p, int nx) {
+  constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, KT = SHORT_KEYS / 32;
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // K, V, per wavefront two tiles of queries
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, 1, sh);
+  const int b = blk.b, h = blk.h;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
+  const CrossRows rows(sh);
+  const int n_keys = visible(sh, p.lens, b), n_sub = (n_keys + 31) / 32, n_rows = rows.count();
+  const int64_t head0 = (int64_t)h * sh.group * D;
+  const float sl2 = LOG2E * sh.scale;
+  bf16_t *ktile = smem, *vtile = smem + 2 * TE, *mine = smem + 4 * TE + wave * 2 * 32 * D;
+  load_states<D, SHORT_KEYS>(sh, p, (int64_t)b * sh.kv_len * sh.kv_stride + h * D, n_keys, ktile, vtile, lane, wave);
+  const RowTiles<D> tiles(rows, (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0, sh.q_stride, lane);
+  bf16_t* out = (bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + head0;
+  const int step = nx * 128;
+  int row0 = blk.x * 128 + wave * 32;
+  if (row0 < n_rows) tiles.issue(mine, row0);
+  wait_loads_and_lds<0>();
+  __syncthreads();
+  for (int stage = 0; row0 < n_rows; row0 += step, stage ^= 1) {
+    bf16_t* qtile = mine + stage * 32 * D;
+    bf16x8_t qf[NS];
+    wait_loads_and_lds<D / 16>();   // (all but the stores of the tile in front, which had 32 rows)
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = frag_rows<D>(qtile, fr_base, 0, s);
+    if (row0 + step < n_rows) tiles.issue(mine + (stage ^ 1) * 32 * D, row0 + step);
+    f32x16_t sc[KT];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      if (i < n_sub) {   // (uniform)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[i][r] = 0.f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) sc[i] = mfma16<F16>(frag_rows<D>(ktile, fr_base, i * 32, s), qf[s], sc[i]);
+        if (32 * i + 32 > n_keys) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[i][r] = 32 * i + acc_row(r, lane) >= n_keys ? -INFINITY : sc[i][r];
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, sc[i][r]);
+      }
+    }
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float mb = m == -INFINITY ? 0.f : m * sl2;
+    f32x16_t o[NT];
+    zero(o);
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      if (i < n_sub) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sc[i][r] = __builtin_amdgcn_exp2f(fmaf(sc[i][r], sl2, -mb));
+          l += sc[i][r];
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8_t pf = pack8<F16>(sc[i], half);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) o[t] = mfma16<F16>(frag_tr<D>(vtile, ft_base, i * 32 + 16 * half, t), pf, o[t]);
+        }
+      }
+    }
+    l += __shfl_xor(l, 32, 64);
+    const float inv = inverse(l);
+    // (through the room of the queries of this tile, which are in registers)
+    static_assert(32 * D >= 16 * RowStage<D, F16>::P, "half a tile of rows");
+    const int my_row = row0 + (lane & 31);
+    RowStage<D, F16>::store_halves(qtile, lane, min(32, n_rows - row0), [&](int t, int e) { return o[t][e] * inv; },
+                                   [&](int r) { return out + rows.at(row0 + r, sh.out_stride, D); });
+    if (p.lse && kc == 0 && my_row < n_rows) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(my_row)] = log_sum(m, l, sh.scale);
+  }
+}
+
+// Backward: dQ, dK and dV of one pass over the queries, five products. Scores and gradients of probabilities have the queries along the lanes, so
+// delta = sum p dP is a lane's own sum (O is not read, and the gradients of scores do not inherit its rounding: with few states they are small
+// differences). dQ^T = K^T dS^T takes them as they are; for dV^T = dO^T P and dK^T = Q^T dS, whose sums run along the queries, P and dS go through
+// a [query][state] tile in LDS, 64 states at a time. dK and dV of the four wavefronts meet in LDS, those of several blocks in cross_sum_kernel.
+// 64-wide heads have two stages of rows and request the next one's at the beginning of a tile, 128-wide ones one, which is free in the middle of it.
+template <int D> constexpr int SHORT_BWD_STAGES = D == 64 ? 2 : 1;
+template <int D> constexpr int SHORT_BWD_KEYS = D == 64 ? 128 : 64;   // as many as leave a wavefront's dK and dV in its registers
+template <int D> constexpr size_t SHORT_BWD_LDS = (2 * SHORT_BWD_KEYS<D> * D + 4 * (2 * SHORT_BWD_STAGES<D> * 32 * D + 2 * 32 * 64)) * sizeof(bf16_t);
+template <int D, bool F16, int KT>
+__global__ __launch_bounds__(256, 1) void cross_bwd_short_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, KEYS = SHORT_BWD_KEYS<D>, NSTG = SHORT_BWD_STAGES<D>, QT = 32 * D, XT = 32 * 64;
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // K, V; per wavefront two stages of queries and dO, and P, dS
+  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, 1, parts.splits, sh);
+  const int b = blk.b, h = blk.h;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane), ft_x = tr_base<64>(lane);
+  const CrossRows rows(sh);
+  const int n_keys = visible(sh, p.lens, b), n_rows = rows.count();
+  const int64_t head0 = (int64_t)h * sh.group * D, stats0 = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
+  const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const float sl2 = LOG2E * sh.scale;
+  bf16_t *ktile = smem, *vtile = smem + KEYS * D, *mine = smem + 2 * KEYS * D + wave * (2 * NSTG * QT + 2 * XT), *pt = mine + 2 * NSTG * QT, *dst = pt + XT;
+  load_states<D, KEYS>(sh, p, kv0, n_keys, ktile, vtile, lane, wave);
+  const RowTiles<D> qtiles(rows, (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0, sh.q_stride, lane);
+  const RowTiles<D> dtiles(rows, (const bf16_t*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0, sh.out_stride, lane);
+  bf16_t* dq_out = (bf16_t*)p.dq + (int64_t)b * sh.q_len * sh.q_stride + head0;
+  f32x16_t dk[KT][NT], dv[KT][NT];
+#pragma unroll
+  for (int i = 0; i < KT; ++i) { zero(dk[i]); zero(dv[i]); }
+  const int step = parts.splits * 128;
+  int row0 = blk.split * 128 + wave * 32;
+  float next_lse = 0.f;
+  auto issue = [&](int stage, int row0) {
+    next_lse = p.lse[stats0 + rows.stat(min(row0 + (lane & 31), n_rows - 1))];
+    qtiles.issue(mine + stage * 2 * QT, row0);
+    dtiles.issue(mine + stage * 2 * QT + QT, row0);
+  };
+  if (row0 < n_rows) issue(0, row0);
+  wait_loads_and_lds<0>();
+  __syncthreads();
+  for (int stage = 0; row0 < n_rows; row0 += step, stage = NSTG - 1 - stage) {
+    bf16_t *qtile = mine + stage * 2 * QT, *dtile = qtile + QT;
+    wait_loads_and_lds<D / 16>();   // (all but the stores of the tile in front, which had 32 rows)
+    asm volatile("" ::: "memory");
+    const float lse2 = next_lse * LOG2E;
+    const bool row_there = row0 + (lane & 31) < n_rows;
+    if (NSTG == 2 && row0 + step < n_rows) issue(stage ^ 1, row0 + step);
+    f32x16_t pr[KT], dp[KT];
+    float delta = 0.f;
+    {
+      bf16x8_t qf[NS], df[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) { qf[s] = frag_rows<D>(qtile, fr_base, 0, s); df[s] = frag_rows<D>(dtile, fr_base, 0, s); }
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pr[i][r] = dp[i][r] = 0.f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          pr[i] = mfma16<F16>(frag_rows<D>(ktile, fr_base, i * 32, s), qf[s], pr[i]);
+          dp[i] = mfma16<F16>(frag_rows<D>(vtile, fr_base, i * 32, s), df[s], dp[i]);
+        }
+        const bool edge = 32 * i + 32 > n_keys || row0 + 32 > n_rows;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pr[i][r] = __builtin_amdgcn_exp2f(fmaf(pr[i][r], sl2, -lse2));
+        if (edge) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) pr[i][r] = row_there && 32 * i + acc_row(r, lane) < n_keys ? pr[i][r] : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) delta = fmaf(pr[i][r], dp[i][r], delta);
+        __builtin_amdgcn_sched_barrier(0);   // (left to itself the scheduler requests the operands of all states at once and spills)
+      }
+    }
+    delta += __shfl_xor(delta, 32, 64);
+    f32x16_t dq[NT];
+    zero(dq);
+    __builtin_amdgcn_sched_barrier(0);
+    // operands whose sums run along the queries: of both halves of 16
+    bf16x8_t tq[2][NT], td[2][NT];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) { tq[half][t] = frag_tr<D>(qtile, ft_base, 16 * half, t); td[half][t] = frag_tr<D>(dtile, ft_base, 16 * half, t); }
+    if (NSTG == 1 && row0 + step < n_rows) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what has been read of the stage has arrived
+      issue(0, row0 + step);
+    }
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[i][r] = pr[i][r] * (dp[i][r] - delta);
+      const bf16x8_t pf[2] = {pack8<F16>(pr[i], 0), pack8<F16>(pr[i], 1)}, dsf[2] = {pack8<F16>(dp[i], 0), pack8<F16>(dp[i], 1)};
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) dq[t] = mfma16<F16>(frag_tr<D>(ktile, ft_base, i * 32 + 16 * half, t), dsf[half], dq[t]);
+      // four states at a time, 8 bytes, into row `lane % 32`: states 32 (i % 2) + 8 c + 4 kc ..
+      const int row = lane & 31, f = Tile<64>::f(row);
+      RowStage<D, F16>::meet();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int at = row * 64 + (((4 * (i & 1) + c) ^ f) << 3) + 4 * kc;
+        const u32x4_t pw = __builtin_bit_cast(u32x4_t, pf[c >> 1]), dw = __builtin_bit_cast(u32x4_t, dsf[c >> 1]);
+        *reinterpret_cast<uint2*>(pt + at) = make_uint2(pw[2 * (c & 1)], pw[2 * (c & 1) + 1]);
+        *reinterpret_cast<uint2*>(dst + at) = make_uint2(dw[2 * (c & 1)], dw[2 * (c & 1) + 1]);
+      }
+      RowStage<D, F16>::meet();
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const bf16x8_t xp = frag_tr<64>(pt, ft_x, 16 * half, i & 1), xd = frag_tr<64>(dst, ft_x, 16 * half, i & 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) { mfma16_agpr<F16>(dv[i][t], td[half][t], xp); mfma16_agpr<F16>(dk[i][t], tq[half][t], xd); }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    static_assert(2 * XT >= 16 * RowStage<D, F16>::P, "half a tile of rows");
+    RowStage<D, F16>::store_halves(pt, lane, min(32, n_rows - row0), [&](int t, int e) { return dq[t][e] * sh.scale; },
+                                   [&](int r) { return dq_out + rows.at(row0 + r, sh.q_stride, D); });
+  }
+  agpr_results_ready();
+  // 32 states at a time: the sums of every wavefront that had rows, and each wavefront adds up a quarter of the registers of all
+  constexpr int QUADS = 2 * NT * 4;   // four registers: four columns
+  float4* slots = reinterpret_cast<float4*>(smem) + lane;
+  const int n_store = (sh.kv_len + 31) / 32, busy = min(4, (n_rows - blk.split * 128 + 31) / 32);
+#pragma unroll
+  for (int i = 0; i < KT; ++i) {
+    if (i >= n_store) break;   // (uniform)
+    __syncthreads();
+    if (wave < busy) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          slots[(wave * QUADS + t * 4 + g) * 64] = make_float4(dk[i][t][4 * g], dk[i][t][4 * g + 1], dk[i][t][4 * g + 2], dk[i][t][4 * g + 3]);
+          slots[(wave * QUADS + (NT + t) * 4 + g) * 64] = make_float4(dv[i][t][4 * g], dv[i][t][4 * g + 1], dv[i][t][4 * g + 2], dv[i][t][4 * g + 3]);
+        }
+    }
+    __syncthreads();
+    const int key = 32 * i + (lane & 31);
+#pragma unroll
+    for (int k = 0; k < QUADS / 4; ++k) {
+      const int quad = wave * (QUADS / 4) + k, array = quad / (4 * NT), col = quad % (4 * NT) * 8 + 4 * kc;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = 0; w < busy; ++w) {
+        const float4 x = slots[(w * QUADS + quad) * 64];
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      }
+      const float factor = array ? 1.f : sh.scale;
+      v = key < n_keys ? make_float4(v.x * factor, v.y * factor, v.z * factor, v.w * factor)
+                       : make_float4(0.f, 0.f, 0.f, 0.f);   // (a row whose gradient is no number must not reach a hidden state)
+      if (key >= sh.kv_len) continue;
+      if (parts.splits > 1) *reinterpret_cast<float4*>(parts.rows<D>(blk.head, sh.batch * sh.kv_heads, blk.split, 2, array, sh.kv_len, key) + col) = v;
+      else *reinterpret_cast<uint2*>((bf16_t*)(array ? p.dv : p.dk) + kv0 + key * sh.kv_stride + col) = make_uint2(pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w));
+    }
+  }
+}
+
 // Adds up the parts of a gradient, in their order, eight columns per thread. QUERY: dq, rows of which are CrossRows; else dk and dv.
 template <int D, bool F16, bool QUERY>
 __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
@@ -859,23 +1160,48 @@ int few_splits(int head_dim, int64_t walk, int64_t heads) {
   }
   return best;
 }
+// Blocks that share the rows of a head (cross_bwd_short_kernel), one at a time on each CU. Estimated in us: 5 for a block's beginning and end, 2.5
+// for 128 rows, 5 for the kernel that adds up the blocks' parts.
+int short_splits(int64_t rows, int64_t heads) {
+  const int64_t tiles = (rows + 127) / 128;
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= MAX_SPLITS && s <= tiles; ++s) {
+    const double t = (double)((heads * s + 255) / 256) * (5.0 + 2.5 * ((tiles + s - 1) / s)) + (s > 1 ? 5.0 : 0.0);
+    if (t < least) { least = t; best = s; }
+  }
+  return best;
+}
+// The same for forward, where blocks leave nothing to add up: as many as the chip holds at a time.
+int short_blocks(int head_dim, int64_t rows, int64_t heads) {
+  const int64_t room = head_dim == 64 ? 512 : 256, tiles = (rows + 127) / 128, most = std::max<int64_t>(1, room / heads);
+  return (int)(tiles < most ? tiles : most);
+}
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-struct FwdPlan { bool few; Form form; size_t o_bytes, total; };
+struct FwdPlan { bool few, one; Form form; size_t o_bytes, total; };
 FwdPlan fwd_plan(int head_dim, const CrossShape& s) {
   FwdPlan f;
   const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
   f.few = rows <= FEW_ROWS;
-  f.form = f.few ? Form{1, 1, few_splits(head_dim, s.kv_len, heads)} : form(rows, s.kv_len, heads);
+  f.one = !f.few && s.kv_len <= SHORT_KEYS;
+  f.form = f.one ? Form{1, short_blocks(head_dim, rows, heads), 1} : f.few ? Form{1, 1, few_splits(head_dim, s.kv_len, heads)} : form(rows, s.kv_len, heads);
   const size_t all = (size_t)(heads * rows * f.form.splits);
   f.o_bytes = f.form.splits > 1 ? up256(all * head_dim * 4) : 0;
   f.total = f.form.splits > 1 ? f.o_bytes + up256(all * 4) : 0;
   return f;
 }
-struct BwdPlan { Form q, kv; size_t delta_bytes, dq_bytes, total; };   // the parts of dq and those of dk and dv share memory one after the other
+struct BwdPlan { bool one; Form q, kv; size_t delta_bytes, total; };   // the parts of dq and those of dk and dv share memory one after the other
 BwdPlan bwd_plan(int head_dim, const CrossShape& s) {
   BwdPlan f;
   const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
+  f.one = s.kv_len <= (head_dim == 64 ? SHORT_BWD_KEYS<64> : SHORT_BWD_KEYS<128>);
+  if (f.one) {
+    f.q = f.kv = Form{1, 1, short_splits(rows, heads)};
+    f.delta_bytes = 0;
+    f.total = f.kv.splits > 1 ? up256((size_t)(heads * s.kv_len * f.kv.splits) * 2 * head_dim * 4) : 256;   // (never 0: one is always passed)
+    return f;
+  }
   f.q = form(rows, s.kv_len, heads);
   f.kv = form(s.kv_len, rows, heads);
   f.delta_bytes = up256((size_t)(heads * rows) * 4);
@@ -899,6 +1225,7 @@ void fwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t);   // K and V
   const int64_t blocks = heads * f.form.nx * f.form.splits;
   if (f.few) launch<64 * FEW_WAVES<D>>(cross_few_kernel<D, F16>, blocks, std::max(FEW_WAVES<D> * tile / 2, (size_t)FEW_WAVES<D> * (D / 2 + 2) * 64 * sizeof(float)), st, s, p, parts);
+  else if (f.one) launch(cross_fwd_short_kernel<D, F16>, blocks, SHORT_FWD_LDS<D>, st, s, p, f.form.nx);
   else if (f.form.groups == 2) launch(cross_fwd_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.form.nx, parts);
   else launch(cross_fwd_kernel<D, F16, 1>, blocks, std::max(2 * tile, (size_t)4 * RowStage<D, F16>::ELEMS * 2), st, s, p, f.form.nx, parts);
   if (f.form.splits > 1) launch(cross_join_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts);
@@ -910,6 +1237,18 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   const int64_t heads = (int64_t)s.batch * s.kv_heads, rows = (int64_t)s.q_len * s.group;
   float *delta = p.ws, *memory = (float*)((char*)p.ws + f.delta_bytes);
   constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t), rows_out = (size_t)4 * RowStage<D, F16>::ELEMS * 2;
+  if (f.one) {
+    const BwdParts parts = {p.ws, f.kv.splits};
+    static_assert(4 * 2 * D * 16 * 4 <= SHORT_BWD_LDS<D>, "dK and dV of 32 states of four wavefronts");
+    const int64_t blocks = heads * f.kv.splits;
+    if (s.kv_len <= 64) launch(cross_bwd_short_kernel<D, F16, 2>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
+    else if constexpr (D == 64) {
+      if (s.kv_len <= 96) launch(cross_bwd_short_kernel<D, F16, 3>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
+      else launch(cross_bwd_short_kernel<D, F16, 4>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
+    }
+    if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16, false>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
+    return;
+  }
   {
     const BwdParts parts = {memory, f.q.splits};
     const int64_t blocks = heads * f.q.nx * f.q.splits;
