@@ -17,23 +17,41 @@ namespace slapo {
 namespace {
 
 // head: of all samples' key heads, sample after sample
-struct CrossBlock { int x, b, h, head, split; };
-// Blocks are handed to the 8 XCDs round-robin in launch order; those of one head are renumbered to sit on one XCD next to each other in time, and
-// share the tiles through its L2. Neighbours of a head are heads of other samples, each key head's list beginning with another sample: samples differ in
-// length, and an XCD or a CU that had all heads of one would be done early or late.
-__device__ __forceinline__ CrossBlock cross_block(unsigned w, unsigned total, int nx, int splits, const CrossShape& sh) {
-  const unsigned xcd = w & 7, q = total >> 3, r = total & 7;
-  w = xcd * q + (xcd < r ? xcd : r) + (w >> 3);
+struct CrossBlock { int x, b, h, head, split; bool none; };
+// The sample with the `rank`-th most visible states (any order among equals, the same in every block).
+__device__ __forceinline__ int sample_by_length(const int32_t* lens, int batch, int rank) {
+  const int lane = threadIdx.x & 63, mine = lane < batch ? lens[lane] : 0;
+  int longer = 0;
+  for (int j = 0; j < batch; ++j) {
+    const int other = __builtin_amdgcn_readlane(mine, j);
+    longer += other > mine || (other == mine && j < lane) ? 1 : 0;
+  }
+  return __builtin_ctzll(__ballot(lane < batch && longer == rank));
+}
+// Which block of the work a workgroup is. Workgroups are handed to the 8 XCDs round-robin in launch order, so (sample, head, split) `unit`s are dealt out
+// to the XCDs in turn, and the nx blocks of a unit sit on one XCD next to each other in time and share the tiles through its L2. Samples of
+// different lengths come longest first; an XCD deals its list out to its 32 CUs, every other time backwards, so that a CU that has begun with a long
+// block gets a short one beside it. Grid: cross_grid.
+template <bool ORDER>
+__device__ __forceinline__ CrossBlock cross_block(int nx, int splits, const CrossShape& sh, const int32_t* lens) {
+  const unsigned units = (unsigned)sh.batch * sh.kv_heads * splits, count = gridDim.x >> 3;   // count: of an XCD
+  unsigned i = blockIdx.x >> 3;
+  const bool order = ORDER && lens && sh.batch > 1 && sh.batch <= 64;
+  if (order && (i & 32) && (i | 31) < count) i ^= 31;
+  unsigned u = i / nx * 8 + (blockIdx.x & 7);
   CrossBlock id;
-  id.x = w % nx;
-  w /= nx;
-  id.split = w % splits;
-  w /= splits;
-  id.h = w / sh.batch;
-  id.b = (w + id.h) % sh.batch;
+  id.none = u >= units;
+  if (id.none) return id;
+  id.x = i % nx;
+  id.split = u % splits;
+  u /= splits;
+  id.h = u % sh.kv_heads;
+  id.b = u / sh.kv_heads;
+  if (order) id.b = sample_by_length(lens, sh.batch, id.b);
   id.head = id.b * sh.kv_heads + id.h;
   return id;
 }
+int64_t cross_grid(const CrossShape& s, int nx, int splits) { return ((int64_t)s.batch * s.kv_heads * splits + 7) / 8 * 8 * nx; }
 // tiles of a split: the walk cut evenly
 __device__ __forceinline__ int split_begin(int n_tiles, int split, int splits) { return (int)((int64_t)n_tiles * split / splits); }
 
@@ -251,7 +269,8 @@ template <int D, bool F16, int G>
 __global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOperands p, int nx, FwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // [2][G][K tile | V tile]
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits, sh);
+  const CrossBlock blk = cross_block<true>(nx, parts.splits, sh, p.lens);
+  if (blk.none) return;
   const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
@@ -351,7 +370,8 @@ template <int D, bool F16>
 __global__ __launch_bounds__(64 * FEW_WAVES<D>) void cross_few_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, TE = 32 * D, WAVES = FEW_WAVES<D>, SPR = D / 8, LOADS = SPR / 2;   // LOADS: wave-level, of 32 rows
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // per wavefront [K tile | V tile]
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, 1, parts.splits, sh);
+  const CrossBlock blk = cross_block<true>(1, parts.splits, sh, p.lens);
+  if (blk.none) return;
   const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
@@ -499,7 +519,8 @@ template <int D, bool F16, int G>
 __global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kernel(CrossShape sh, CrossOperands p, int nx, float* __restrict__ delta, BwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // [2][G][K tile | V tile]
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits, sh);
+  const CrossBlock blk = cross_block<true>(nx, parts.splits, sh, p.lens);
+  if (blk.none) return;
   const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
@@ -640,7 +661,8 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
   constexpr int FB = 4;                 // k-steps of fragment prefetch
   constexpr bool ACC_A = D == 128;      // dK/dV accumulators in AGPRs (see mfma16_agpr)
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, parts.splits, sh);
+  const CrossBlock blk = cross_block<true>(nx, parts.splits, sh, p.lens);
+  if (blk.none) return;
   const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int row_wave = wave % (4 / G), grp = G == 1 ? 0 : wave / (4 / G);
@@ -874,7 +896,8 @@ template <int D, bool F16>
 __global__ __launch_bounds__(256) void cross_fwd_short_kernel(CrossShape sh, CrossOperands p, int nx) {
   constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, KT = SHORT_KEYS / 32;
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // K, V, per wavefront two tiles of queries
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, nx, 1, sh);
+  const CrossBlock blk = cross_block<true>(nx, 1, sh, p.lens);
+  if (blk.none) return;
   const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
@@ -959,7 +982,8 @@ template <int D, bool F16, int KT>
 __global__ __launch_bounds__(256, 1) void cross_bwd_short_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, KEYS = SHORT_BWD_KEYS<D>, NSTG = SHORT_BWD_STAGES<D>, QT = 32 * D, XT = 32 * 64;
   extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // K, V; per wavefront two stages of queries and dO, and P, dS
-  const CrossBlock blk = cross_block(blockIdx.x, gridDim.x, 1, parts.splits, sh);
+  const CrossBlock blk = cross_block<true>(1, parts.splits, sh, p.lens);
+  if (blk.none) return;
   const int b = blk.b, h = blk.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
   const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane), ft_x = tr_base<64>(lane);
@@ -1223,7 +1247,7 @@ void fwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   const int64_t heads = (int64_t)s.batch * s.kv_heads, rows = (int64_t)s.q_len * s.group;
   const FwdParts parts = {p.ws, (float*)((char*)p.ws + f.o_bytes), f.form.splits};
   constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t);   // K and V
-  const int64_t blocks = heads * f.form.nx * f.form.splits;
+  const int64_t blocks = cross_grid(s, f.form.nx, f.form.splits);
   if (f.few) launch<64 * FEW_WAVES<D>>(cross_few_kernel<D, F16>, blocks, std::max(FEW_WAVES<D> * tile / 2, (size_t)FEW_WAVES<D> * (D / 2 + 2) * 64 * sizeof(float)), st, s, p, parts);
   else if (f.one) launch(cross_fwd_short_kernel<D, F16>, blocks, SHORT_FWD_LDS<D>, st, s, p, f.form.nx);
   else if (f.form.groups == 2) launch(cross_fwd_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.form.nx, parts);
@@ -1240,7 +1264,7 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   if (f.one) {
     const BwdParts parts = {p.ws, f.kv.splits};
     static_assert(4 * 2 * D * 16 * 4 <= SHORT_BWD_LDS<D>, "dK and dV of 32 states of four wavefronts");
-    const int64_t blocks = heads * f.kv.splits;
+    const int64_t blocks = cross_grid(s, 1, f.kv.splits);
     if (s.kv_len <= 64) launch(cross_bwd_short_kernel<D, F16, 2>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
     else if constexpr (D == 64) {
       if (s.kv_len <= 96) launch(cross_bwd_short_kernel<D, F16, 3>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
@@ -1251,14 +1275,14 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   }
   {
     const BwdParts parts = {memory, f.q.splits};
-    const int64_t blocks = heads * f.q.nx * f.q.splits;
+    const int64_t blocks = cross_grid(s, f.q.nx, f.q.splits);
     if (f.q.groups == 2) launch(cross_dq_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.q.nx, delta, parts);
     else launch(cross_dq_kernel<D, F16, 1>, blocks, std::max(2 * tile, rows_out), st, s, p, f.q.nx, delta, parts);
     if (f.q.splits > 1) launch(cross_sum_kernel<D, F16, true>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts);
   }
   {
     const BwdParts parts = {memory, f.kv.splits};
-    const int64_t blocks = heads * f.kv.nx * f.kv.splits;
+    const int64_t blocks = cross_grid(s, f.kv.nx, f.kv.splits);
     constexpr size_t stage = tile + 512, meet = (size_t)2 * D * 2 * 64 * sizeof(float);   // two wavefronts' dK and dV
     if (f.kv.groups == 2) launch(cross_dkdv_kernel<D, F16, 2>, blocks, std::max(4 * stage, meet), st, s, p, f.kv.nx, (const float*)delta, parts);
     else launch(cross_dkdv_kernel<D, F16, 1>, blocks, std::max(2 * stage, rows_out), st, s, p, f.kv.nx, (const float*)delta, parts);
