@@ -1156,15 +1156,21 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOper
 // What a launch looks like: groups of wavefronts per block, blocks along the rows, splits of the walk.
 struct Form { int groups, nx, splits; };
 
-// `rows` own rows of each of `heads` heads, a walk of `walk` others
-Form form(int64_t rows, int64_t walk, int64_t heads) {
+// `rows` own rows of each of `heads` heads, a walk of `walk` others.
+// Two groups, i.e. blocks of 64 rows that take two tiles at a time: 64-wide heads while blocks of 128 rows are at most one per CU (two of those with two
+// groups fit one), 128-wide ones, whose two groups fill the LDS of a CU, while those of 64 rows are. us, one group / two: 64-wide, forward 2 x 512
+// rows, 1024 states, 16 heads (128 blocks of 128) 19.8 / 13.1; 5 x 1143, 777, 4 (180) 14.1 / 11.6; 8 x 512, 1024, 16 (512) 24.1 / 28.9; dQ and dK/dV of
+// the second 51.3 / 36.2, of the third 75.7 / 79.7; 128-wide, forward 1 x 1024, 1024, 20 heads (320 blocks of 64) 26.2 / 34.7, dQ and dK/dV 67 / 90.
+// Splits of the walk, which a second kernel adds up (5 to 10 us): while the blocks are far fewer than the CUs and the walk is long. 1 x 128 rows, 8192 states, 16
+// heads of 128 in 2 / 4 / 8 splits 58.9 / 37.4 / 29.7; 1 x 512, 4096, 16 of 64 (128 blocks) in 1 / 2 / 4 26.3 / 26.2 / 25.6.
+Form form(int head_dim, int64_t rows, int64_t walk, int64_t heads) {
   Form f;
-  const int64_t tiles = (walk + 63) / 64;
-  f.groups = ((rows + 63) / 64) * heads <= 256 && tiles > 1 ? 2 : 1;
+  const int64_t tiles = (walk + 63) / 64, wide = (rows + 127) / 128 * heads, narrow = (rows + 63) / 64 * heads;
+  f.groups = (head_dim == 64 ? wide : narrow) <= 256 && tiles > 1 ? 2 : 1;
   f.nx = (int)((rows + 128 / f.groups - 1) / (128 / f.groups));
   const int64_t blocks = f.nx * heads;
   f.splits = 1;
-  while (f.splits < MAX_SPLITS && blocks * f.splits * 2 <= 256 && tiles >= 4 * f.groups * f.splits) f.splits *= 2;
+  while (f.splits < MAX_SPLITS && blocks * f.splits <= 128 && tiles >= 4 * f.groups * f.splits) f.splits *= 2;
   return f;
 }
 constexpr int FEW_ROWS = 32;
@@ -1209,7 +1215,7 @@ FwdPlan fwd_plan(int head_dim, const CrossShape& s) {
   const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
   f.few = rows <= FEW_ROWS;
   f.one = !f.few && s.kv_len <= SHORT_KEYS;
-  f.form = f.one ? Form{1, short_blocks(head_dim, rows, heads), 1} : f.few ? Form{1, 1, few_splits(head_dim, s.kv_len, heads)} : form(rows, s.kv_len, heads);
+  f.form = f.one ? Form{1, short_blocks(head_dim, rows, heads), 1} : f.few ? Form{1, 1, few_splits(head_dim, s.kv_len, heads)} : form(head_dim, rows, s.kv_len, heads);
   const size_t all = (size_t)(heads * rows * f.form.splits);
   f.o_bytes = f.form.splits > 1 ? up256(all * head_dim * 4) : 0;
   f.total = f.form.splits > 1 ? f.o_bytes + up256(all * 4) : 0;
@@ -1226,8 +1232,8 @@ BwdPlan bwd_plan(int head_dim, const CrossShape& s) {
     f.total = f.kv.splits > 1 ? up256((size_t)(heads * s.kv_len * f.kv.splits) * 2 * head_dim * 4) : 256;   // (never 0: one is always passed)
     return f;
   }
-  f.q = form(rows, s.kv_len, heads);
-  f.kv = form(s.kv_len, rows, heads);
+  f.q = form(head_dim, rows, s.kv_len, heads);
+  f.kv = form(head_dim, s.kv_len, rows, heads);
   f.delta_bytes = up256((size_t)(heads * rows) * 4);
   const size_t dq = f.q.splits > 1 ? (size_t)(heads * rows * f.q.splits) * head_dim * 4 : 0;
   const size_t dkv = f.kv.splits > 1 ? (size_t)(heads * s.kv_len * f.kv.splits) * 2 * head_dim * 4 : 0;
