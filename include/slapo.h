@@ -389,7 +389,7 @@ typedef struct {
  * accepted: the sum is 0. SLAPO_ERR_WORKSPACE: no host memory for the check. */
 typedef struct {
   void *memory;
-  int64_t n, segments, segment;
+  int64_t segments;                         /* of all arrays */
 } slapo_grad_plan;
 int slapo_grad_plan_bytes(int32_t n, const slapo_grad *grads, size_t *bytes);
 int slapo_grad_plan_build(int32_t n, const slapo_grad *grads, void *memory, slapo_grad_plan *plan, void *stream);

@@ -47,7 +47,7 @@ class _Grad(C.Structure):
 
 
 class _GradPlan(C.Structure):
-    _fields_ = [("memory", C.c_void_p), ("n", C.c_int64), ("segments", C.c_int64), ("segment", C.c_int64)]
+    _fields_ = [("memory", C.c_void_p), ("segments", C.c_int64)]
 
 
 class SlapoError(RuntimeError):

@@ -81,37 +81,25 @@ int check_rope_axes(const slapo_rope_axes_desc* d) {
 }
 
 // ---- gradient norm ----------------------------------------------------------------------------------------
-// Bytes of a segment: about two segments for each of the blocks that run, between 8 and 64 KB (a segment costs a block two dependent
-// look-ups in front of its first element).
-int64_t grad_segment(int64_t bytes) {
-  int64_t s = 8192;
-  while (s < 65536 && bytes / s > 2 * GRAD_BLOCKS) s *= 2;
-  return s;
-}
-inline int64_t grad_segments(const slapo_grad& g, int64_t segment) {
-  const int64_t per = segment / element_bytes(g.dtype);
+inline int64_t grad_segments(const slapo_grad& g) {
+  const int64_t per = GRAD_SEGMENT / element_bytes(g.dtype);
   return (g.count + per - 1) / per;
 }
 // Checks the arrays and counts their segments.
-int check_grads(int32_t n, const slapo_grad* grads, bool pointers, int64_t* segments, int64_t* segment) {
+int check_grads(int32_t n, const slapo_grad* grads, bool pointers, int64_t* segments) {
   if (n < 0) return SLAPO_ERR_SHAPE;
   if (n > 0 && !grads) return SLAPO_ERR_NULL;
-  int64_t bytes = 0;
+  *segments = 0;
   for (int i = 0; i < n; ++i) {
     const slapo_grad& g = grads[i];
     if (!known_dtype(g.dtype)) return SLAPO_ERR_UNSUPPORTED;
     if (g.count < 0) return SLAPO_ERR_SHAPE;
-    if (g.count >= ((int64_t)1 << 40) || bytes >= ((int64_t)1 << 48)) return SLAPO_ERR_UNSUPPORTED;
-    bytes += g.count * element_bytes(g.dtype);
+    if (g.count >= ((int64_t)1 << 40)) return SLAPO_ERR_UNSUPPORTED;
+    *segments += grad_segments(g);
+    if (*segments >= ((int64_t)1 << 31)) return SLAPO_ERR_UNSUPPORTED;
     if (!pointers || g.count == 0) continue;
     if (!g.grad) return SLAPO_ERR_NULL;
     if (misaligned(g.grad) || misaligned(g.out)) return SLAPO_ERR_ALIGN;
-  }
-  *segment = grad_segment(bytes);
-  *segments = 0;
-  for (int i = 0; i < n; ++i) {
-    *segments += grad_segments(grads[i], *segment);
-    if (*segments >= ((int64_t)1 << 31)) return SLAPO_ERR_UNSUPPORTED;
   }
   return SLAPO_OK;
 }
@@ -139,7 +127,7 @@ int check_shared_memory(int32_t n, const slapo_grad* grads) {
 }
 int check_plan(const slapo_grad_plan* p) {
   if (!p || !p->memory) return SLAPO_ERR_NULL;
-  if (p->n < 0 || p->segments < 0 || p->segment < 8192) return SLAPO_ERR_SHAPE;
+  if (p->segments < 0 || p->segments >= ((int64_t)1 << 31)) return SLAPO_ERR_SHAPE;
   return SLAPO_OK;
 }
 
@@ -216,30 +204,30 @@ int slapo_rope_axes(const slapo_rope_axes_desc* d, const int32_t* positions, con
 
 int slapo_grad_plan_bytes(int32_t n, const slapo_grad* grads, size_t* bytes) {
   if (!bytes) return SLAPO_ERR_NULL;
-  int64_t segments, segment;
-  const int rc = check_grads(n, grads, false, &segments, &segment);
+  int64_t segments;
+  const int rc = check_grads(n, grads, false, &segments);
   if (rc) return rc;
-  *bytes = grad_plan_layout(n, segments).total;
+  *bytes = grad_plan_layout(segments).total;
   return SLAPO_OK;
 }
 
 int slapo_grad_plan_build(int32_t n, const slapo_grad* grads, void* memory, slapo_grad_plan* plan, void* stream) {
-  int64_t segments, segment;
-  int rc = check_grads(n, grads, true, &segments, &segment);
+  int64_t segments;
+  int rc = check_grads(n, grads, true, &segments);
   if (rc) return rc;
   if (!memory || !plan) return SLAPO_ERR_NULL;
   if (misaligned(memory)) return SLAPO_ERR_ALIGN;
   try {
     if ((rc = check_shared_memory(n, grads))) return rc;
-    std::vector<GradEntry> entries((size_t)n);
+    std::vector<GradArray> arrays((size_t)n);
     int64_t first = 0;
     for (int i = 0; i < n; ++i) {
-      entries[i] = {grads[i].grad, grads[i].out ? grads[i].out : const_cast<void*>(grads[i].grad), grads[i].count, grads[i].dtype, (int32_t)first};
-      first += grad_segments(grads[i], segment);
+      arrays[i] = {grads[i].grad, grads[i].out ? grads[i].out : const_cast<void*>(grads[i].grad), grads[i].count, first, grads[i].dtype};
+      first += grad_segments(grads[i]);
     }
-    *plan = {memory, n, segments, segment};
+    *plan = {memory, segments};
     entry_error();
-    launch_grad_plan(n, entries.data(), segments, segment, memory, (hipStream_t)stream);
+    launch_grad_plan(n, arrays.data(), memory, (hipStream_t)stream);
   } catch (const std::bad_alloc&) {   // (host memory for a table of the arrays)
     return SLAPO_ERR_WORKSPACE;
   }
@@ -252,7 +240,7 @@ int slapo_grad_sumsq(const slapo_grad_plan* plan, int accumulate, double* sumsq,
   if (!sumsq) return SLAPO_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(sumsq) & 7u) != 0) return SLAPO_ERR_ALIGN;
   entry_error();
-  launch_grad_sumsq(plan->n, plan->segments, plan->segment, plan->memory, accumulate ? 1 : 0, sumsq, (hipStream_t)stream);
+  launch_grad_sumsq(plan->segments, plan->memory, accumulate ? 1 : 0, sumsq, (hipStream_t)stream);
   return finish();
 }
 
@@ -263,7 +251,7 @@ int slapo_grad_clip(const slapo_grad_plan* plan, const double* sumsq, float max_
   if (!(max_norm > 0.f)) return SLAPO_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(sumsq) & 7u) != 0 || (reinterpret_cast<uintptr_t>(norm) & 3u) != 0) return SLAPO_ERR_ALIGN;
   entry_error();
-  launch_grad_clip(plan->n, plan->segments, plan->segment, plan->memory, sumsq, max_norm, norm, (hipStream_t)stream);
+  launch_grad_clip(plan->segments, plan->memory, sumsq, max_norm, norm, (hipStream_t)stream);
   return finish();
 }
 

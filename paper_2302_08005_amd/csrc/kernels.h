@@ -168,19 +168,24 @@ struct RopeAxes {
 };
 void launch_rope_axes(int dtype, const RopeAxes& r, const int32_t* positions, const void* in, void* out, hipStream_t st);
 
-// Sums of squares and scaling over many arrays (grad_norm.hip). An array is cut into segments of `segment` bytes; the plan's device
-// memory holds a counter, an entry per array, the array of each segment, and a partial sum per block.
-struct GradEntry {
+// Sums of squares and scaling over many arrays (grad_norm.hip). The arrays are cut into segments; a plan's device memory holds a
+// counter, the segments, and a partial sum per block.
+struct GradArray {
   const void* in;
   void* out;
-  int64_t count;
-  int32_t dtype, first;   // first: its first segment
+  int64_t count, first;   // first: its first segment
+  int32_t dtype;
 };
-constexpr int GRAD_BLOCKS = 2048;
-struct GradPlanLayout { size_t entries, map, partials, total; };
-GradPlanLayout grad_plan_layout(int64_t n, int64_t segments);
-void launch_grad_plan(int n, const GradEntry* entries, int64_t segments, int64_t segment, void* memory, hipStream_t st);
-void launch_grad_sumsq(int64_t n, int64_t segments, int64_t segment, void* memory, int accumulate, double* sumsq, hipStream_t st);
-void launch_grad_clip(int64_t n, int64_t segments, int64_t segment, void* memory, const double* sumsq, float max_norm, float* norm, hipStream_t st);
+struct GradSegment {
+  const void* in;
+  void* out;
+  int32_t count, dtype;
+};
+constexpr int64_t GRAD_SEGMENT = 32768;   // bytes
+struct GradPlanLayout { size_t segments, partials, total; };
+GradPlanLayout grad_plan_layout(int64_t segments);
+void launch_grad_plan(int n, const GradArray* arrays, void* memory, hipStream_t st);
+void launch_grad_sumsq(int64_t segments, void* memory, int accumulate, double* sumsq, hipStream_t st);
+void launch_grad_clip(int64_t segments, void* memory, const double* sumsq, float max_norm, float* norm, hipStream_t st);
 
 }  // namespace slapo

@@ -99,7 +99,7 @@ def test_gradient_plans():
     assert L.slapo_grad_plan_build(*grads((P, None, 8, f)), None, C.byref(plan), None) == -1
     assert L.slapo_grad_plan_build(*grads((P, None, 8, f)), P + 8, C.byref(plan), None) == -4
     assert L.slapo_grad_plan_build(*grads((P, None, 8, f)), P, None, None) == -1
-    good = B._GradPlan(P, 1, 1, 8192)
+    good = B._GradPlan(P, 1)
     assert L.slapo_grad_sumsq(None, 0, P, None) == -1 and L.slapo_grad_sumsq(C.byref(B._GradPlan()), 0, P, None) == -1
     assert L.slapo_grad_sumsq(C.byref(good), 0, None, None) == -1 and L.slapo_grad_sumsq(C.byref(good), 0, P + 4, None) == -4
     assert L.slapo_grad_clip(C.byref(good), P, 0.0, None, None) == -2 and L.slapo_grad_clip(C.byref(good), P, float("nan"), None, None) == -2
