@@ -44,7 +44,7 @@ __device__ __forceinline__ f32x4_t rows_times_rows(const RowFrags<D>& a, const R
 // row lane % 16 of w. x(row): element of this lane's column in that row; rows from n on (to the next multiple of 16) count as zeros.
 template <class X>
 __device__ __forceinline__ f32x4_t weighted_rows(f32x4_t acc, const float* w, int n, int g, X&& x) {
-  constexpr int U = 4;   // tiles of 16 rows in flight: the walk is a chain of load latencies
+  constexpr int U = CHUNK / 16;   // tiles of 16 rows in flight, all of a chunk: the walk is a chain of load latencies
   for (int t0 = 0; t0 < n; t0 += 16 * U) {
     float v[U][4];
 #pragma unroll
