@@ -326,8 +326,8 @@ int slapo_dropout_mask(const slapo_layer_desc *desc, int site, int64_t T, uint8_
  * values the halves of one (v = k + kv_heads * head_dim, kv_stride = 2 * kv_heads * head_dim) or of the projections of several
  * decoder layers side by side; samples follow each other, len * stride apart. Columns between the rows are left alone.
  * Sizes: head_dim 64 or 128; heads a multiple of kv_heads; strides multiples of 8; of each array a sample (and 256 tokens more) below 2^31
- * bytes; batch and heads at most 65535; rows = q_len * heads / kv_heads below 2^26, and batch * kv_heads times 64-row tiles of the
- * longer of rows and kv_len below 2^23. */
+ * bytes; batch and heads at most 65535; rows = q_len * heads / kv_heads below 2^26; batch * kv_heads below 2^21, and
+ * times the 64-row tiles of the longer of rows and kv_len below 2^23. */
 typedef struct {
   int32_t batch, q_len, kv_len, heads, kv_heads, head_dim;
   int32_t dtype;                            /* SLAPO_BF16 | SLAPO_FP32 | SLAPO_FP16: q, k, v, out and their gradients */

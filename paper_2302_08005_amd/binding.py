@@ -426,7 +426,7 @@ class GradPlan:
         need = C.c_size_t(0)
         _check(lib().slapo_grad_plan_bytes(len(grads), table, C.byref(need)), "slapo_grad_plan_bytes")
         self.memory = torch.empty(need.value, dtype=torch.uint8, device=f"cuda:{self.device}")
-        self.tensors, self.plan = (grads, out), _GradPlan()
+        self.tensors, self.plan, self.stream = (grads, out), _GradPlan(), st
         _check(lib().slapo_grad_plan_build(len(grads), table, self.memory.data_ptr(), C.byref(self.plan), st), "slapo_grad_plan_build")
 
 
@@ -438,19 +438,24 @@ def _scalar(name, t, dtype, device, optional=False):
     return t.data_ptr()
 
 
-def slapo_grad_sumsq(plan: GradPlan, sumsq, accumulate=0, stream=None):
-    """sumsq: one float64."""
+def _plan_stream(plan, stream):
     st, dev = _stream_and_device(stream)
     if dev != plan.device:
         raise ValueError(f"the plan belongs to device {plan.device}, the stream to {dev}")
+    if st != plan.stream:   # (torch must not hand the plan's memory to others while this stream uses it)
+        plan.memory.record_stream(stream if stream is not None else torch.cuda.current_stream(dev))
+    return st, dev
+
+
+def slapo_grad_sumsq(plan: GradPlan, sumsq, accumulate=0, stream=None):
+    """sumsq: one float64."""
+    st, dev = _plan_stream(plan, stream)
     _check(lib().slapo_grad_sumsq(C.byref(plan.plan), accumulate, _scalar("sumsq", sumsq, torch.float64, dev), st), "slapo_grad_sumsq")
 
 
 def slapo_grad_clip(plan: GradPlan, sumsq, max_norm, norm=None, stream=None):
     """norm: one float32, or None."""
-    st, dev = _stream_and_device(stream)
-    if dev != plan.device:
-        raise ValueError(f"the plan belongs to device {plan.device}, the stream to {dev}")
+    st, dev = _plan_stream(plan, stream)
     _check(lib().slapo_grad_clip(C.byref(plan.plan), _scalar("sumsq", sumsq, torch.float64, dev), max_norm,
                                  _scalar("norm", norm, torch.float32, dev, True), st), "slapo_grad_clip")
 

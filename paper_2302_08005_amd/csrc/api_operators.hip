@@ -32,9 +32,10 @@ int check_cross(const slapo_cross_attn_desc* d) {
     // a sample's offsets are 32-bit, also those of the rows of a last tile that reach beyond it
     if ((a.stride > a.width ? a.stride : a.width) * element_bytes(d->dtype) * (a.tokens + 256) >= ((int64_t)1 << 31)) return SLAPO_ERR_UNSUPPORTED;
   }
-  // (launch dimensions: blocks of 16 fp32 rows in one, blocks of 64 rows of all heads in one)
+  // (launch dimensions: blocks of 16 fp32 rows in one; blocks of 64 rows of all heads, and 1024 threads for each head, in one)
   const int64_t rows = (int64_t)d->q_len * (d->heads / d->kv_heads);
   if (rows >= ((int64_t)1 << 26)) return SLAPO_ERR_UNSUPPORTED;
+  if ((int64_t)d->batch * d->kv_heads >= ((int64_t)1 << 21)) return SLAPO_ERR_UNSUPPORTED;
   if ((int64_t)d->batch * d->kv_heads * ((std::max(rows, (int64_t)d->kv_len) + 63) / 64) >= ((int64_t)1 << 23)) return SLAPO_ERR_UNSUPPORTED;
   return SLAPO_OK;
 }

@@ -208,9 +208,11 @@ struct Softmax {
   f32x16_t o[NT];
   float m = -INFINITY, l = 0.f;   // what probabilities are relative to (raw scores), sum of this lane's half
   __device__ __forceinline__ Softmax() { zero(o); }
+  // GROWN in raw scores; finite, so that the first tile always moves m from -infinity
+  static __device__ __forceinline__ float grown(float sl2) { return fminf(GROWN / sl2, 3e38f); }
   // 32-row sub-tiles of scores -> probabilities
   template <int SUBS>
-  __device__ __forceinline__ void add(f32x16_t (&sc)[SUBS], float sl2, float grown) {   // grown: GROWN / sl2
+  __device__ __forceinline__ void add(f32x16_t (&sc)[SUBS], float sl2, float grown) {
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < SUBS; ++i)
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(256) void cross_fwd_kernel(CrossShape sh, CrossOper
   const int first = split_begin(all_tiles, blk.split, parts.splits), n_tiles = split_begin(all_tiles, blk.split + 1, parts.splits) - first;
   const int wave_row = blk.x * RB + 32 * row_wave, my_row = wave_row + (lane & 31);
   const int64_t head0 = (int64_t)h * sh.group * D;
-  const float sl2 = LOG2E * sh.scale, grown = Softmax<D>::GROWN / sl2;
+  const float sl2 = LOG2E * sh.scale, grown = Softmax<D>::grown(sl2);
 
   const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
   bf16x8_t qf[NS];
@@ -380,7 +382,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES<D>) void cross_few_kernel(CrossShape
   const int first = split_begin(all_tiles, blk.split, parts.splits) + wave, end = split_begin(all_tiles, blk.split + 1, parts.splits);
   const int my_row = lane & 31;
   const int64_t head0 = (int64_t)h * sh.group * D;
-  const float sl2 = LOG2E * sh.scale, grown = Softmax<D>::GROWN / sl2;
+  const float sl2 = LOG2E * sh.scale, grown = Softmax<D>::grown(sl2);
 
   bf16_t *ktile = smem + wave * 2 * TE, *vtile = ktile + TE;
   const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
@@ -1213,8 +1215,8 @@ struct FwdPlan { bool few, one; Form form; size_t o_bytes, total; };
 FwdPlan fwd_plan(int head_dim, const CrossShape& s) {
   FwdPlan f;
   const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
-  f.few = rows <= FEW_ROWS;
-  f.one = !f.few && s.kv_len <= SHORT_KEYS;
+  f.one = s.kv_len <= SHORT_KEYS;
+  f.few = !f.one && rows <= FEW_ROWS;
   f.form = f.one ? Form{1, short_blocks(head_dim, rows, heads), 1} : f.few ? Form{1, 1, few_splits(head_dim, s.kv_len, heads)} : form(head_dim, rows, s.kv_len, heads);
   const size_t all = (size_t)(heads * rows * f.form.splits);
   f.o_bytes = f.form.splits > 1 ? up256(all * head_dim * 4) : 0;

@@ -19,7 +19,8 @@ def test_cross_attention_descriptor():
     for kw, status in ((dict(batch=0), -2), (dict(q_len=0), -2), (dict(kv_len=-1), -2), (dict(kv_heads=3), -2), (dict(kv_heads=0), -2), (dict(head_dim=32), -3),
                        (dict(dtype=5), -3), (dict(scale=-1.0), -2), (dict(scale=float("nan")), -2), (dict(scale=float("inf")), -2), (dict(q_stride=248), -2),
                        (dict(q_stride=260), -4), (dict(kv_stride=120), -2), (dict(kv_stride=-256), -2), (dict(out_stride=257), -4),
-                       (dict(kv_len=1 << 23), -3), (dict(q_len=1 << 24), -3), (dict(batch=70000), -3), (dict(kv_len=4096, kv_stride=1 << 20), -3)):
+                       (dict(kv_len=1 << 23), -3), (dict(q_len=1 << 24), -3), (dict(batch=70000), -3), (dict(kv_len=4096, kv_stride=1 << 20), -3),
+                       (dict(batch=60000, heads=64, kv_heads=64), -3), (dict(q_len=1 << 22, heads=32), -3)):
         with pytest.raises(B.SlapoError) as e:
             B.slapo_cross_attn_workspace(cross(**kw))
         assert e.value.status == status, (kw, e.value.status)

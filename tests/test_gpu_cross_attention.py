@@ -116,8 +116,22 @@ def test_every_length_around_a_tile(dtype):
     Problem(70, 3, 69, 2, 1, 64, dtype=dtype, lens=list(range(70))).check()
 
 
+@pytest.mark.parametrize("width", [64, 128])
+@pytest.mark.parametrize("kv_len", [31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 191, 192])
+def test_lengths_around_the_forms_of_the_kernels(kv_len, width):
+    for q_len, heads, kv_heads in ((31, 2, 2), (33, 2, 2), (8, 12, 3), (130, 3, 1)):
+        Problem(2, q_len, kv_len, heads, kv_heads, width, lens=[kv_len, kv_len - 1], strided=True).check()
+
+
+@pytest.mark.parametrize("batch", [63, 64, 65])
+def test_batches_around_those_that_are_ordered_by_length(batch):
+    """Blocks of samples of several lengths are put in order up to 64 samples: every sample is still computed once."""
+    Problem(batch, 2, 300, 2, 1, 64, lens=[(37 * i) % 301 for i in range(batch)]).check()
+    Problem(batch, 40, 140, 1, 1, 64, lens=[140 - (i % 3) * 70 for i in range(batch)]).check()
+
+
 @pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
-@pytest.mark.parametrize("scale", [0.01, 1.0])
+@pytest.mark.parametrize("scale", [1e-38, 0.01, 1.0])
 def test_scales(dtype, scale):
     Problem(2, 70, 150, 4, 2, 64, dtype=dtype, scale=scale, lens=[150, 99]).check()
 
@@ -210,3 +224,70 @@ def test_on_another_stream_and_replayed():
         p.backward()
         for a, b in zip(got, (p.out, p.lse, p.dq, p.dk, p.dv)):
             assert torch.equal(a, b), i
+
+
+def test_samples_whose_states_lie_beyond_32_bits():
+    """Three samples of 2.1 GB of states each, columns of a wide array: the last ones against 64-bit products on the device."""
+    batch, kv_len, stride, w = 3, 65000, 16384, 64
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    kv = torch.empty((batch, kv_len, stride), dtype=torch.bfloat16, device=DEV)
+    kv[..., -2 * w:] = torch.randn((batch, kv_len, 2 * w), device=DEV, generator=gen)
+    k, v = kv[..., -2 * w:-w], kv[..., -w:]
+    for q_len in (1, 70):
+        d = B.make_cross_attn_desc(batch=batch, q_len=q_len, kv_len=kv_len, heads=1, head_dim=w, kv_stride=stride)
+        q = torch.randn((batch, q_len, w), device=DEV, generator=gen).to(torch.bfloat16)
+        out, lse = torch.empty_like(q), torch.empty((batch, 1, q_len), device=DEV)
+        need = B.slapo_cross_attn_workspace(d)
+        ws = torch.empty(max(need), dtype=torch.uint8, device=DEV)
+        B.slapo_cross_attn_fwd(d, q, k, v, None, out, lse, ws)
+        dkv = torch.empty_like(kv)
+        dq, dk, dv = torch.empty_like(q), dkv[..., -2 * w:-w], dkv[..., -w:]
+        do = torch.randn(q.shape, device=DEV, generator=gen).to(torch.bfloat16)
+        B.slapo_cross_attn_bwd(d, q, k, v, None, out, do, lse, dq, dk, dv, ws)
+        for b in range(batch):
+            p = torch.softmax(q[b].double() @ k[b].double().t().contiguous() / 8, 1)
+            want = p @ v[b].double()
+            # (u of the result and of the probabilities: sum p |v| is below 1 here, sqrt(2 / pi) on average; 1.1 for the 32-bit sums)
+            assert bool(((out[b].double() - want).abs() <= 2.0 ** -8 * 1.1 * (want.abs() + p @ v[b].double().abs())).all())
+            wdv = p.t().contiguous() @ do[b].double()
+            assert bool(((dv[b].double() - wdv).abs() <= 2.0 ** -8 * 1.1 * (wdv.abs() + p.t().contiguous() @ do[b].double().abs())).all())
+        del dkv
+
+
+def test_two_streams_at_once_and_two_graphs_with_one_workspace():
+    """Calls side by side have a workspace each; graphs that are replayed one after the other may share one."""
+    a, b = Problem(2, 33, 900, 4, 2, 64, lens=[900, 77]), Problem(3, 5, 2100, 8, 2, 64, seed=5)
+    want = []
+    for p in (a, b):
+        p.forward()
+        p.backward()
+        want.append([x.clone() for x in (p.out, p.lse, p.dq, p.dk, p.dv)])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for p, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                p.forward()
+                p.backward()
+    torch.cuda.synchronize()
+    for p, w in zip((a, b), want):
+        assert all(torch.equal(x, y) for x, y in zip((p.out, p.lse, p.dq, p.dk, p.dv), w))
+    n = max(x.numel() for p in (a, b) for x in p.ws if x is not None)
+    shared = torch.empty(n, dtype=torch.uint8, device=DEV)
+    graphs = []
+    for p in (a, b):
+        p.ws = [shared, shared]
+        p.forward()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            p.forward()
+            p.backward()
+        graphs.append(g)
+    for _ in range(3):
+        for p, g, w in zip((a, b), graphs, want):
+            for x in (p.out, p.lse, p.dq, p.dk, p.dv):
+                x.fill_(3.0)
+            g.replay()
+        torch.cuda.synchronize()
+        for p, w in zip((a, b), want):
+            assert all(torch.equal(x, y) for x, y in zip((p.out, p.lse, p.dq, p.dk, p.dv), w))

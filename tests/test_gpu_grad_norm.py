@@ -163,3 +163,33 @@ def test_refused():
             B.slapo_grad_clip(plan, s, bad)
     with pytest.raises(ValueError):
         B.slapo_grad_sumsq(plan, s.float())
+
+
+def test_an_array_of_more_than_2_31_elements():
+    """Sum and clipped values of its last elements: 2^31 + 77 of 1/2, and one of 3 behind them."""
+    n = 2 ** 31 + 77
+    g = torch.full((n + 1,), 0.5, dtype=torch.bfloat16, device=DEV)
+    g[n] = 3.0
+    plan = B.GradPlan([g])
+    s, norm = torch.empty(1, dtype=torch.float64, device=DEV), torch.empty(1, device=DEV)
+    B.slapo_grad_sumsq(plan, s)
+    assert s.item() == n / 4 + 9.0   # (exact in 64 bits)
+    B.slapo_grad_clip(plan, s, 1.0, norm)
+    want = 1.0 / s.item() ** 0.5
+    tail = g[-100:].double()
+    assert bool(((tail[:-1] - 0.5 * want).abs() <= 0.5 * want * 2.0 ** -8 * 1.01).all()) and abs(tail[-1].item() - 3 * want) <= 3 * want * 2.0 ** -8 * 1.01
+    assert bool((g[:-1] == g[0]).all())
+
+
+def test_on_another_stream_than_the_plan_was_built_on():
+    g = arrays([100000, 3], [torch.float32])
+    before = [x.clone() for x in g]
+    side = torch.cuda.Stream()
+    s, norm = torch.empty(1, dtype=torch.float64, device=DEV), torch.empty(1, device=DEV)
+    plan = B.GradPlan(g)
+    side.wait_stream(torch.cuda.current_stream())
+    B.slapo_grad_sumsq(plan, s, stream=side)
+    with torch.cuda.stream(side):
+        B.slapo_grad_clip(plan, s, 1.0, norm)
+    torch.cuda.current_stream().wait_stream(side)
+    check(g, g, s.item(), norm.item(), 1.0, before)

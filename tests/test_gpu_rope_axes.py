@@ -102,3 +102,17 @@ def test_refused_tensors():
     with pytest.raises(B.SlapoError) as e:   # in and out share memory without being the same rows
         B.slapo_rope_axes(B.make_rope_axes_desc(6, 2, 64, (16, 16), in_stride=136, out_stride=136), dpos, flat[:6 * 136].view(6, 136), flat[8:].view(6, 136))
     assert e.value.status == -2
+
+
+def test_rows_beyond_32_bits():
+    """40000 rows of 65536 elements: 5.2 GB in, the last rows against the definition."""
+    rows, stride = 40000, 65536
+    back = torch.empty((rows, stride), dtype=torch.bfloat16, device=DEV)
+    x = store(np.random.default_rng(2).standard_normal((rows, 64)), W.BF16)
+    back[:, :64] = torch.from_numpy(x).to(DEV)
+    pos = np.random.default_rng(3).integers(0, 100000, (rows, 2)).astype(np.int32)
+    y = torch.empty((rows, 64), dtype=torch.bfloat16, device=DEV)
+    B.slapo_rope_axes(B.make_rope_axes_desc(rows, 1, 64, (16, 16), in_stride=stride), torch.from_numpy(pos).to(DEV), back, y)
+    x = x.astype(np.float64).reshape(rows, 1, 64)
+    want = O.rotary(x, pos, (16, 16))
+    assert (np.abs(to_np(y).reshape(want.shape) - want) <= O.rotary_bound(x, want, pos, (16, 16), ROUND[W.BF16], TINY[W.BF16])).all()
