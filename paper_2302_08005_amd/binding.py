@@ -396,12 +396,16 @@ def slapo_rope_axes(desc, positions, x, out, inverse=0, stream=None):
 def _rows(name, t, dtype, rows, width, stride, device):
     """Address of a tensor of `rows` rows of at least `width` elements, `stride` apart."""
     shape, strides = t.shape, t.stride()
-    ok = t.dtype is dtype and t.is_cuda and t.get_device() == device and len(shape) >= 1 and shape[-1] >= width and strides[-1] == 1
-    n = 1
-    for size, step in zip(reversed(shape[:-1]), reversed(strides[:-1])):
-        ok = ok and (size == 1 or step == n * stride)
-        n *= size
-    if not ok or n != rows:
+    ok = t.dtype is dtype and t.is_cuda and t.get_device() == device and shape[-1] >= width and strides[-1] == 1
+    if len(shape) == 2:
+        ok = ok and shape[0] == rows and (rows == 1 or strides[0] == stride)
+    else:
+        n = 1
+        for size, step in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+            ok = ok and (size == 1 or step == n * stride)
+            n *= size
+        ok = ok and n == rows
+    if not ok:
         _refuse(name, t, f"{dtype}, {rows} rows of {width} or more elements, {stride} from one to the next,")
     return t.data_ptr()
 

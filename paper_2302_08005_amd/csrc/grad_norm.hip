@@ -10,6 +10,8 @@ namespace slapo {
 
 namespace {
 
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
 constexpr int TABLE = 64;   // arrays that one launch cuts into a plan's segments
 struct GradTable { GradArray a[TABLE]; };
 
@@ -97,14 +99,29 @@ __global__ __launch_bounds__(SUM_THREADS) void grad_sumsq_kernel(int64_t n, cons
   if (threadIdx.x == 0) *sumsq = (accumulate ? *sumsq : 0.0) + t;
 }
 
-template <typename T>
+// Eight elements past the caches.
+__device__ __forceinline__ void store8_past(bf16_t* p, const float (&v)[8]) {
+  const u32x4_t w = {pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3]), pack2<false>(v[4], v[5]), pack2<false>(v[6], v[7])};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(p));
+}
+__device__ __forceinline__ void store8_past(f16_t* p, const float (&v)[8]) {
+  const u32x4_t w = {pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3]), pack2<true>(v[4], v[5]), pack2<true>(v[6], v[7])};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(p));
+}
+__device__ __forceinline__ void store8_past(float* p, const float (&v)[8]) {
+  __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_t*>(p));
+  __builtin_nontemporal_store(f32x4_t{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_t*>(p + 4));
+}
+
+template <bool PAST, typename T>
 __device__ __forceinline__ void scale_segment(const T* in, T* out, int n, float factor, float step) {
   const auto put = [&](int i, const Raw8<T>& r) {
     float v[8];
     r.get(v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = v[k] * step * factor;
-    store8(out + i, v);
+    if constexpr (PAST) store8_past(out + i, v);
+    else store8(out + i, v);
   };
   int i = 8 * threadIdx.x;
   for (; i + 8 * 256 * (IN_FLIGHT - 1) + 8 <= n; i += 8 * 256 * IN_FLIGHT) {
@@ -122,7 +139,11 @@ __device__ __forceinline__ void scale_segment(const T* in, T* out, int n, float 
   for (; i < n; ++i) from_f32(out[i], to_f32(in[i]) * step * factor);
 }
 
-// Segments are taken from the last to the first: the sums were taken the other way round, and what they read last the caches still hold.
+// Segments are taken from the last to the first: the sums were taken the other way round, and what they read last the caches still hold. PAST: what is
+// written goes past them, and does not drive out what is still to be read. From PAST_FROM segments (64 MB in, 64 MB out) on; below, whoever reads the
+// clipped gradients next finds them there. Sums and clipping, bf16, cached / past: 302M values 350 / 321 us, 50M 61.5 / 52.5, 25M 31.8 / 31.8.
+constexpr int64_t PAST_FROM = 2048;
+template <bool PAST>
 __global__ __launch_bounds__(256) void grad_clip_kernel(int64_t n, const GradSegment* __restrict__ segments, const double* __restrict__ sumsq, float max_norm,
                                                         float* __restrict__ norm_out) {
   const double norm = sqrt(*sumsq);
@@ -134,9 +155,9 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(int64_t n, const GradSeg
   for (int64_t i = n - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
     const GradSegment g = segments[i];
     if (!scaled && g.in == g.out) continue;
-    if (g.dtype == DT_FP32) scale_segment((const float*)g.in, (float*)g.out, g.count, factor, step);
-    else if (g.dtype == DT_FP16) scale_segment((const f16_t*)g.in, (f16_t*)g.out, g.count, factor, step);
-    else scale_segment((const bf16_t*)g.in, (bf16_t*)g.out, g.count, factor, step);
+    if (g.dtype == DT_FP32) scale_segment<PAST>((const float*)g.in, (float*)g.out, g.count, factor, step);
+    else if (g.dtype == DT_FP16) scale_segment<PAST>((const f16_t*)g.in, (f16_t*)g.out, g.count, factor, step);
+    else scale_segment<PAST>((const bf16_t*)g.in, (bf16_t*)g.out, g.count, factor, step);
   }
 }
 
@@ -172,7 +193,7 @@ void launch_grad_sumsq(int64_t segments, void* memory, int accumulate, double* s
 
 void launch_grad_clip(int64_t segments, void* memory, const double* sumsq, float max_norm, float* norm, hipStream_t st) {
   const GradPlanLayout L = grad_plan_layout(segments);
-  hipLaunchKernelGGL(grad_clip_kernel, dim3(grad_grid(segments, 2048)), dim3(256), 0, st, segments, (const GradSegment*)((char*)memory + L.segments), sumsq,
+  hipLaunchKernelGGL(segments >= PAST_FROM ? grad_clip_kernel<true> : grad_clip_kernel<false>, dim3(grad_grid(segments, 2048)), dim3(256), 0, st, segments, (const GradSegment*)((char*)memory + L.segments), sumsq,
                      max_norm, norm);
 }
 

@@ -193,3 +193,17 @@ def test_on_another_stream_than_the_plan_was_built_on():
         B.slapo_grad_clip(plan, s, 1.0, norm)
     torch.cuda.current_stream().wait_stream(side)
     check(g, g, s.item(), norm.item(), 1.0, before)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_many_megabytes(in_place):
+    """Beyond 64 MB what is written goes past the caches: every type, with ends that fill no segment; against 64 bits on the device."""
+    grads = [torch.randn(n, device=DEV).to(t) for n, t in ((17 * 2 ** 20 + 5, torch.float32), (9 * 2 ** 20 + 1, torch.bfloat16), (8 * 2 ** 20 - 3, torch.float16))]
+    before = [g.clone() for g in grads]
+    out = None if in_place else [torch.zeros_like(g) for g in grads]
+    sumsq, norm = clip(grads, out, 3.0)
+    want = sum(b.double().square().sum() for b in before).item()
+    assert abs(sumsq - want) <= 1e-12 * want and abs(norm - want ** 0.5) <= 2.0 ** -24 * 1.0001 * want ** 0.5
+    for b, c in zip(before, grads if in_place else out):
+        w = b.double() * (3.0 / want ** 0.5)
+        assert bool(((c.double() - w).abs() <= w.abs() * (HALF_STEP[c.dtype] + 3 * 2.0 ** -24) + TINY[c.dtype]).all())
