@@ -394,39 +394,46 @@ __global__ __launch_bounds__(64 * FEW_WAVES<D>) void cross_few_kernel(CrossShape
     const int slot = i * 64 + lane, row = slot / SPR, pos = slot % SPR;
     voff[i] = (unsigned)(row * sh.kv_stride * 2) + (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
   }
-  auto issue = [&](int t) {
+  // the room of K is free again behind the scores, that of V behind the outputs, and either is asked for the next tile at once
+  auto issue = [&](const bf16_t* x, bf16_t* tile, int t) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wavefront has read of the tile in front has arrived
     const unsigned at = (unsigned)t * step;
 #pragma unroll
-    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(k, bytes, ktile + n * 512, voff[n] + at, 0);
-#pragma unroll
-    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(v, bytes, vtile + n * 512, voff[n] + at, 0);
+    for (int n = 0; n < LOADS; ++n) buffer_load_lds_16_untracked(x, bytes, tile + n * 512, voff[n] + at, 0);
   };
-  if (first < end) issue(first);
+  if (first < end) {
+    issue(k, ktile, first);
+    issue(v, vtile, first);
+  }
   const bf16_t* q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(min(my_row, n_rows - 1), sh.q_stride, D);
   bf16x8_t qf[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(q + 16 * s + 8 * kc);
   Softmax<D> sm;
   for (int t = first; t < end; t += WAVES) {
-    wait_loads_and_lds<0>();
+    const bool more = t + WAVES < end;
+    wait_loads_and_lds<LOADS>();   // all but V's (and, of the first tile, those of the queries, which the compiler waits for)
     asm volatile("" ::: "memory");
     f32x16_t sc[1];
     zero(sc);
 #pragma unroll
     for (int s = 0; s < NS; ++s) sc[0] = mfma16<F16>(frag_rows<D>(ktile, fr_base, 0, s), qf[s], sc[0]);
+    if (more) issue(k, ktile, t + WAVES);
     if (32 * t + 32 > n_keys) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[0][r] = 32 * t + acc_row(r, lane) >= n_keys ? -INFINITY : sc[0][r];
     }
     sm.add(sc, sl2, grown);
+    if (more) wait_loads_and_lds<LOADS>();   // all but the next tile's K
+    else wait_loads_and_lds<0>();
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const bf16x8_t pf = pack8<F16>(sc[0], half);
 #pragma unroll
       for (int c = 0; c < NT; ++c) sm.o[c] = mfma16<F16>(frag_tr<D>(vtile, ft_base, 16 * half, c), pf, sm.o[c]);
     }
-    if (t + WAVES < end) issue(t + WAVES);
+    if (more) issue(v, vtile, t + WAVES);
   }
   // every wavefront puts some of the accumulators of all together: registers REGS w .. of the 16 NT
   __syncthreads();
@@ -473,24 +480,27 @@ __global__ __launch_bounds__(64 * FEW_WAVES<D>) void cross_few_kernel(CrossShape
   }
 }
 
-// Puts the splits of a row together, by their logsumexps: eight columns per thread.
+// Puts the splits of a row together, by their logsumexps: eight columns per thread; `groups` threads share the splits of a row, one or two each as far as
+// a block's threads go, and put theirs together through LDS.
 constexpr int MAX_SPLITS = 64;
+template <int D> constexpr int JOIN_GROUPS = 256 / (D / 8);   // at most
 template <int D, bool F16>
-__global__ __launch_bounds__(256) void cross_join_kernel(CrossShape sh, CrossOperands p, FwdParts parts) {
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossShape sh, CrossOperands p, FwdParts parts, int groups) {
   constexpr int C = D / 8;
+  __shared__ float4 sums[2 * 256];
+  __shared__ float2 stats[256];
   const CrossRows rows(sh);
-  const int n_rows = rows.count();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / C;
-  if (row >= (int64_t)sh.batch * sh.kv_heads * n_rows) return;
-  const int head = (int)(row / n_rows), r = (int)(row - (int64_t)head * n_rows), b = head / sh.kv_heads, h = head - b * sh.kv_heads, c = 8 * (int)(i % C);
+  const int n_rows = rows.count(), tid = threadIdx.x, c = 8 * (tid % C), g = tid / C % groups;
+  const int64_t all = (int64_t)sh.batch * sh.kv_heads * n_rows, row = (int64_t)blockIdx.x * (256 / (C * groups)) + tid / (C * groups);
+  const int64_t my_row = row < all ? row : all - 1;
+  const int head = (int)(my_row / n_rows), r = (int)(my_row - (int64_t)head * n_rows), b = head / sh.kv_heads, h = head - b * sh.kv_heads;
   const float* lse = parts.stat(head, 0, n_rows, r);
   const float* src = parts.rows<D>(head, 0, n_rows, r) + c;
-  float m = -INFINITY;
-  for (int s = 0; s < parts.splits; ++s) m = fmaxf(m, lse[(int64_t)s * n_rows]);
+  float m = -INFINITY, total = 0.f, o[8] = {};
+  for (int s = g; s < parts.splits; s += groups) m = fmaxf(m, lse[(int64_t)s * n_rows]);
   const float base = m == -INFINITY ? 0.f : m;
-  float total = 0.f, o[8] = {};
-#pragma unroll 4
-  for (int s = 0; s < parts.splits; ++s) {
+#pragma unroll 2
+  for (int s = g; s < parts.splits; s += groups) {
     const float weight = __expf(lse[(int64_t)s * n_rows] - base);
     float v[8];
     load8(src + (int64_t)s * n_rows * D, v);
@@ -498,11 +508,32 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossShape sh, CrossOpe
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = fmaf(weight, v[e], o[e]);
   }
+  for (int half = groups >> 1; half > 0; half >>= 1) {
+    if (g >= half && g < 2 * half) {
+      stats[tid] = make_float2(m, total);
+      sums[tid] = make_float4(o[0], o[1], o[2], o[3]);
+      sums[256 + tid] = make_float4(o[4], o[5], o[6], o[7]);
+    }
+    __syncthreads();
+    if (g < half) {
+      const int other = tid + half * C;
+      const float2 st = stats[other];
+      const float4 x = sums[other], y = sums[256 + other];
+      const float theirs[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      const float top = fmaxf(m, st.x), from = top == -INFINITY ? 0.f : top, wm = __expf(m - from), wt = __expf(st.x - from);
+      total = total * wm + st.y * wt;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = o[e] * wm + theirs[e] * wt;
+      m = top;
+    }
+    __syncthreads();
+  }
+  if (g != 0 || row >= all) return;
   const float inv = inverse(total);
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] *= inv;
   store8h<F16>((bf16_t*)p.o + (int64_t)b * sh.q_len * sh.out_stride + (int64_t)h * sh.group * D + rows.at(r, sh.out_stride, D) + c, o);
-  if (p.lse && c == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(r)] = total != 0.f ? base + __logf(total) : -INFINITY;
+  if (p.lse && c == 0) p.lse[((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(r)] = log_sum(m, total, 1.f);
 }
 
 // ======================================== backward ======================================================
@@ -1177,7 +1208,7 @@ Form form(int head_dim, int64_t rows, int64_t walk, int64_t heads) {
 }
 constexpr int FEW_ROWS = 32;
 // Blocks that share a walk over the states. Estimated in us, for what a block at a time on each CU takes: 3 for a block's beginning and end, for
-// every step of its wavefronts over tiles (128 KB) what a CU's rate of reading (37 GB/s) or the memory's (5.9 TB/s) takes, 4 for the second kernel.
+// every step of its wavefronts over tiles (128 KB) what a CU's rate of reading (37 GB/s) or the memory's (5.9 TB/s) takes, 5 for the second kernel.
 // Measured for 1 / 2 / 4 / 8: 16 samples x 16384 states, 8 key heads of 128 242 / 182 / 187 / 198 (estimate 227 / 189 / 193 / 198); 8 x 1024, 16 of 64
 // 11.0 / 12.9 / 16.4.
 int few_splits(int head_dim, int64_t walk, int64_t heads) {
@@ -1187,7 +1218,7 @@ int few_splits(int head_dim, int64_t walk, int64_t heads) {
   for (int s = 1; s <= MAX_SPLITS && (s == 1 || tiles >= waves * s); ++s) {
     const int64_t blocks = heads * s, rounds = (blocks + 255) / 256, steps = (tiles + waves * s - 1) / (waves * s);
     const double step = std::max(131072 / 37e3, (blocks < 256 ? blocks : 256) * (131072 / 5.9e6));
-    const double t = rounds * (3.0 + steps * step) + (s > 1 ? 4.0 : 0.0);
+    const double t = rounds * (3.0 + steps * step) + (s > 1 ? 5.0 : 0.0);
     if (t < least) { least = t; best = s; }
   }
   return best;
@@ -1260,7 +1291,11 @@ void fwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   else if (f.one) launch(cross_fwd_short_kernel<D, F16>, blocks, SHORT_FWD_LDS<D>, st, s, p, f.form.nx);
   else if (f.form.groups == 2) launch(cross_fwd_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.form.nx, parts);
   else launch(cross_fwd_kernel<D, F16, 1>, blocks, std::max(2 * tile, (size_t)4 * RowStage<D, F16>::ELEMS * 2), st, s, p, f.form.nx, parts);
-  if (f.form.splits > 1) launch(cross_join_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts);
+  if (f.form.splits > 1) {
+    int groups = 1;
+    while (groups < JOIN_GROUPS<D> && 2 * groups < f.form.splits) groups *= 2;
+    launch(cross_join_kernel<D, F16>, (heads * rows * (D / 8) * groups + 255) / 256, 0, st, s, p, parts, groups);
+  }
 }
 
 template <int D, bool F16>
