@@ -685,6 +685,15 @@ __global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kern
   RowStage<D, F16>::store(stage, lane, min(32, n_rows - wave_row), value, [&](int r) { return out + rows.at(wave_row + r, sh.q_stride, D); });
 }
 
+// The end of a step's products into the accumulation registers. The compiler does not know them for matrix instructions (see mfma16_agpr) and waits for
+// none; where an accumulator has another register on the next path it moves it, and a move right behind the product reads a sum that is not there yet.
+// What is moved behind this statement is its results, and it waits longer than any product takes.
+template <int NT>
+__device__ __forceinline__ void settle(f32x16_t (&dk)[NT], f32x16_t (&dv)[NT]) {
+  if constexpr (NT == 4) {
+    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(dk[0]), "+a"(dk[1]), "+a"(dk[2]), "+a"(dk[3]), "+a"(dv[0]), "+a"(dv[1]), "+a"(dv[2]), "+a"(dv[3]));
+  }
+}
 // dK and dV of 128 / G states; those of hidden states are zeros.
 template <int D, bool F16, int G>
 __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_kernel(CrossShape sh, CrossOperands p, int nx, const float* __restrict__ delta, BwdParts parts) {
@@ -705,7 +714,7 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
   const int all_tiles = kv_base < n_keys ? (n_rows + 63) / 64 : 0;   // nothing to do for hidden states
   const int first = split_begin(all_tiles, blk.split, parts.splits), n_tiles = split_begin(all_tiles, blk.split + 1, parts.splits) - first;
   const int wave_key = kv_base + 32 * row_wave, my_key = wave_key + (lane & 31);
-  const bool seen = my_key < n_keys, key_edge = wave_key + 32 > n_keys;
+  const bool seen = my_key < n_keys;
   const int64_t head0 = (int64_t)h * sh.group * D, stats0 = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
   const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   const float sl2 = LOG2E * sh.scale;
@@ -728,7 +737,13 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
   const float* stat_src = ((tid & 127) < 64 ? p.lse : delta) + stats0;
   const float stat_mul = (tid & 127) < 64 ? LOG2E : 1.0f;
   const int stat_tile = (tid >> 7) % G;
-  auto load_stats = [&](int step) { return stat_src[rows.stat(min((first + step * G + stat_tile) * 64 + (tid & 63), n_rows - 1))]; };
+  // Nothing in the loop is masked. Rows behind the last one arrive as zeros and get an lse of infinity, which makes their p zero; a hidden state's
+  // column is its lane's own in every product, and is not stored.
+  auto load_stats = [&](int step) {
+    const int row = (first + step * G + stat_tile) * 64 + (tid & 63);
+    const float v = stat_src[rows.stat(min(row, n_rows - 1))];
+    return row >= n_rows && (tid & 127) < 64 ? INFINITY : v;
+  };
   auto store_stats = [&](int stage, float v) { reinterpret_cast<float*>(smem + stage * STAGE + stat_tile * TILE + 2 * TE)[tid & 127] = v * stat_mul; };
   QueryTiles<D> tiles(rows, (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0, sh.q_stride,
                       (const bf16_t*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0, sh.out_stride, first * 64, lane, wave);
@@ -739,21 +754,20 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
       tiles.issue(smem + stage * STAGE + g * TILE, smem + stage * STAGE + g * TILE + TE);
     }
   };
-  auto compute = [&](int stage, int step) {
-    if (G > 1 && step * G + grp >= n_tiles) return;
-    const int q0 = (first + step * G + grp) * 64;
+  auto compute = [&](int stage, int step, auto last) {
+    if constexpr (G > 1 && decltype(last)::value) {
+      if (step * G + grp >= n_tiles) return;
+    }
     const bf16_t* qtile = smem + stage * STAGE + grp * TILE;
     const bf16_t* dtile = qtile + TE;
     const float* stat = reinterpret_cast<const float*>(qtile + 2 * TE);
     if constexpr (D == 128 && G == 1) {   // (two groups' tiles leave no registers for it)
-      if (!key_edge && q0 + 64 <= n_rows) {   // no mask boundary
-        dkdv_interior<F16>(qtile, dtile, stat, kf, vf, dk, dv, fr_base, ft_base, kc, sl2);
-        return;
-      }
+      dkdv_interior<F16>(qtile, dtile, stat, kf, vf, dk, dv, fr_base, ft_base, kc, sl2);
+      settle(dk, dv);
+      return;
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int qs = q0 + i * 32;
       f32x16_t sc, dp;
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[r] = dp[r] = 0.f;
@@ -783,24 +797,18 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
         tq0[t] = frag_tr<D>(qtile, ft_base, i * 32, t);
       }
       __builtin_amdgcn_sched_barrier(0);
-      auto elements = [&](auto edge) {   // (two instances: interior tiles carry no mask code)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float4 l4 = *reinterpret_cast<const float4*>(stat + i * 32 + g * 8 + 4 * kc);
-          const float4 d4 = *reinterpret_cast<const float4*>(stat + 64 + i * 32 + g * 8 + 4 * kc);
-          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
+      for (int g = 0; g < 4; ++g) {
+        const float4 l4 = *reinterpret_cast<const float4*>(stat + i * 32 + g * 8 + 4 * kc);
+        const float4 d4 = *reinterpret_cast<const float4*>(stat + 64 + i * 32 + g * 8 + 4 * kc);
+        const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * g + e;
-            float pr = __builtin_amdgcn_exp2f(fmaf(sc[r], sl2, -ls[e]));
-            if (decltype(edge)::value) pr = (!seen | (qs + g * 8 + 4 * kc + e >= n_rows)) ? 0.f : pr;
-            sc[r] = pr;
-            dp[r] = pr * (dp[r] - ds[e]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], sl2, -ls[e]));
+          dp[r] = sc[r] * (dp[r] - ds[e]);
         }
-      };
-      if (key_edge || qs + 32 > n_rows) elements(std::true_type{});
-      else elements(std::false_type{});
+      }
       const bf16x8_t pf0 = pack8<F16>(sc, 0), dsf0 = pack8<F16>(dp, 0), pf1 = pack8<F16>(sc, 1), dsf1 = pack8<F16>(dp, 1);
       __builtin_amdgcn_sched_barrier(0);
       bf16x8_t td1[NT], tq1[NT];   // second half's operands, requested in front of the first half's MFMAs
@@ -823,6 +831,7 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    if (ACC_A) settle(dk, dv);
   };
   // Two stages: step it + 1 is requested while step it is computed; its statistics travel through registers and are requested before its tile
   // loads, so that waiting for them leaves those in flight.
@@ -833,23 +842,19 @@ __global__ __launch_bounds__(256, D == 64 && G == 1 ? 2 : 1) void cross_dkdv_ker
     store_stats(0, stat0);
     wait_loads_and_lds<0>();
     block_barrier();
-    for (int it0 = 0; it0 < n_steps; it0 += 2) {
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const int it = it0 + st;
-        if (it >= n_steps) break;   // uniform
-        const bool more = it + 1 < n_steps;
-        float next = 0.f;
-        if (more) {
-          next = load_stats(it + 1);
-          issue_step(st ^ 1, it + 1);
-        }
-        compute(st, it);
-        if (more) store_stats(st ^ 1, next);
-        wait_loads_and_lds<0>();
-        block_barrier();
-      }
+    int it = 0;
+    for (; it + 1 < n_steps; ++it) {
+      const int st = it & 1;
+      const float next = load_stats(it + 1);
+      issue_step(st ^ 1, it + 1);
+      compute(st, it, std::false_type{});
+      store_stats(st ^ 1, next);
+      wait_loads_and_lds<0>();
+      block_barrier();
     }
+    compute(it & 1, it, std::true_type{});
+    wait_loads_and_lds<0>();
+    block_barrier();
   }
   if (ACC_A) agpr_results_ready();
   if constexpr (G > 1) {   // (behind the last barrier: the stages are free)

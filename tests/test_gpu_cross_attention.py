@@ -116,6 +116,13 @@ def test_every_length_around_a_tile(dtype):
     Problem(70, 3, 69, 2, 1, 64, dtype=dtype, lens=list(range(70))).check()
 
 
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("shape", [(2, 300, 900, 20, 20, 128), (3, 700, 800, 16, 16, 64), (1, 1100, 1300, 24, 8, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_lengths_inside_a_group_of_states_with_blocks_for_every_unit(shape, dtype):
+    """Enough blocks of the widest kind: the states end inside a wavefront's 32, and rows inside the last tile."""
+    Problem(*shape, dtype=dtype, lens=[shape[2] - 47, 513, 500]).check()
+
+
 @pytest.mark.parametrize("width", [64, 128])
 @pytest.mark.parametrize("kv_len", [31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 191, 192])
 def test_lengths_around_the_forms_of_the_kernels(kv_len, width):
