@@ -153,13 +153,24 @@ __global__ __launch_bounds__(256) void cross_fwd_f32_kernel(CrossShape sh, Cross
   }
 }
 
-// dQ of 16 rows; also leaves delta = rowsum(dO * O) of its rows in p.ws, laid out as lse, for the other kernel.
+// delta = rowsum(dO * O) of the row lane % 16, in all lanes that hold a share of it
 template <int D>
-__global__ __launch_bounds__(256) void cross_dq_f32_kernel(CrossShape sh, CrossOperands p) {
-  __shared__ __attribute__((aligned(16))) float grad[16 * PITCH];
-  __shared__ float delta[16];
+__device__ __forceinline__ float delta_of(const RowFrags<D>& dout, const RowFrags<D>& out) {
+  float d = 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    d = fmaf(dout.v[c].x, out.v[c].x, d); d = fmaf(dout.v[c].y, out.v[c].y, d);
+    d = fmaf(dout.v[c].z, out.v[c].z, d); d = fmaf(dout.v[c].w, out.v[c].w, d);
+  }
+  d += __shfl_xor(d, 16, 64);
+  return d + __shfl_xor(d, 32, 64);
+}
+
+// dQ of the 16 rows of block x. LEAVE: also leaves their delta in p.ws, laid out as lse.
+template <int D, bool LEAVE>
+__device__ __forceinline__ void dq_f32(const CrossShape& sh, const CrossOperands& p, int x, float* grad) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-  const int b = blockIdx.z, h = blockIdx.y, r0 = blockIdx.x * 16;
+  const int b = blockIdx.z, h = blockIdx.y, r0 = x * 16;
   const CrossRows rows(sh);
   const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), my_row = min(r0 + i, n_rows - 1);
   const int64_t head0 = (int64_t)h * sh.group * D, stats = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
@@ -172,15 +183,8 @@ __global__ __launch_bounds__(256) void cross_dq_f32_kernel(CrossShape sh, CrossO
   df.load((const float*)p.dout + out0, g, true);
   of.load((const float*)p.out + out0, g, true);
   const float lse = p.lse[stats + rows.stat(my_row)];
-  float my_delta = 0.f;
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c) {
-    my_delta = fmaf(df.v[c].x, of.v[c].x, my_delta); my_delta = fmaf(df.v[c].y, of.v[c].y, my_delta);
-    my_delta = fmaf(df.v[c].z, of.v[c].z, my_delta); my_delta = fmaf(df.v[c].w, of.v[c].w, my_delta);
-  }
-  my_delta += __shfl_xor(my_delta, 16, 64);
-  my_delta += __shfl_xor(my_delta, 32, 64);
-  if (wave == 0 && g == 0 && r0 + i < n_rows) p.ws[stats + rows.stat(my_row)] = my_delta;
+  const float my_delta = delta_of(df, of);
+  if (LEAVE && wave == 0 && g == 0 && r0 + i < n_rows) p.ws[stats + rows.stat(my_row)] = my_delta;
   constexpr int MINE = D / 64;
   f32x4_t acc[MINE];
 #pragma unroll
@@ -217,17 +221,17 @@ __global__ __launch_bounds__(256) void cross_dq_f32_kernel(CrossShape sh, CrossO
   }
 }
 
-// dK and dV of 16 states; hidden ones get zeros.
-template <int D>
-__global__ __launch_bounds__(256) void cross_dkdv_f32_kernel(CrossShape sh, CrossOperands p) {
-  __shared__ __attribute__((aligned(16))) float prob[16 * PITCH], grad[16 * PITCH];
+// dK and dV of the 16 states of block x; hidden ones get zeros. OWN: takes delta of its own, else finds it in p.ws.
+template <int D, bool OWN>
+__device__ __forceinline__ void dkdv_f32(const CrossShape& sh, const CrossOperands& p, int x, float* prob, float* grad) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-  const int b = blockIdx.z, h = blockIdx.y, k0 = blockIdx.x * 16;
+  const int b = blockIdx.z, h = blockIdx.y, k0 = x * 16;
   const CrossRows rows(sh);
   const int n_keys = visible(sh, p.lens, b), n_rows = k0 < n_keys ? rows.count() : 0;
   const int64_t head0 = (int64_t)h * sh.group * D, stats = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len;
   const float* q = (const float*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0;
-  const float* dout = (const float*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0;
+  const int64_t out0 = (int64_t)b * sh.q_len * sh.out_stride + head0;
+  const float* dout = (const float*)p.dout + out0;
   const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   const bool seen = k0 + i < n_keys;
   RowFrags<D> kf, vf;
@@ -244,6 +248,12 @@ __global__ __launch_bounds__(256) void cross_dkdv_f32_kernel(CrossShape sh, Cros
       RowFrags<D> qf, df;
       qf.load(q + rows.at(at, sh.q_stride, D), g, row < n_rows);
       df.load(dout + rows.at(at, sh.out_stride, D), g, row < n_rows);
+      float row_delta = 0.f;
+      if constexpr (OWN) {
+        RowFrags<D> of;
+        of.load((const float*)p.out + out0 + rows.at(at, sh.out_stride, D), g, row < n_rows);
+        row_delta = delta_of(df, of);
+      }
       const f32x4_t s = rows_times_rows<D>(qf, kf), dp = rows_times_rows<D>(df, vf);
       f32x4_t pv, ds;
 #pragma unroll
@@ -252,7 +262,8 @@ __global__ __launch_bounds__(256) void cross_dkdv_f32_kernel(CrossShape sh, Cros
         const int64_t stat = stats + rows.stat(min(r0 + mine, n_rows - 1));
         const float e = seen && mine < n ? __expf(s[r] * sh.scale - p.lse[stat]) : 0.f;
         pv[r] = e;
-        ds[r] = seen && mine < n ? e * (dp[r] - p.ws[stat]) : 0.f;
+        const float delta = OWN ? __shfl(row_delta, 4 * g + r, 64) : p.ws[stat];
+        ds[r] = seen && mine < n ? e * (dp[r] - delta) : 0.f;
       }
       *reinterpret_cast<f32x4_t*>(prob + i * PITCH + 16 * t + 4 * g) = pv;
       *reinterpret_cast<f32x4_t*>(grad + i * PITCH + 16 * t + 4 * g) = ds;
@@ -280,15 +291,40 @@ __global__ __launch_bounds__(256) void cross_dkdv_f32_kernel(CrossShape sh, Cros
 }
 
 template <int D>
+__global__ __launch_bounds__(256) void cross_dq_f32_kernel(CrossShape sh, CrossOperands p) {
+  __shared__ __attribute__((aligned(16))) float grad[16 * PITCH];
+  dq_f32<D, true>(sh, p, blockIdx.x, grad);
+}
+template <int D>
+__global__ __launch_bounds__(256) void cross_dkdv_f32_kernel(CrossShape sh, CrossOperands p) {
+  __shared__ __attribute__((aligned(16))) float prob[16 * PITCH], grad[16 * PITCH];
+  dkdv_f32<D, false>(sh, p, blockIdx.x, prob, grad);
+}
+// Both in one launch: a third operand to read for the blocks of states, nothing to wait for.
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_bwd_f32_kernel(CrossShape sh, CrossOperands p, int key_blocks) {
+  __shared__ __attribute__((aligned(16))) float prob[16 * PITCH], grad[16 * PITCH];
+  if ((int)blockIdx.x < key_blocks) dkdv_f32<D, true>(sh, p, blockIdx.x, prob, grad);   // (the longer ones first)
+  else dq_f32<D, false>(sh, p, blockIdx.x - key_blocks, grad);
+}
+
+template <int D>
 void fwd_f32(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   const unsigned blocks = (unsigned)(((int64_t)s.q_len * s.group + 15) / 16);
   hipLaunchKernelGGL((cross_fwd_f32_kernel<D>), dim3(blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
 }
 template <int D>
 void bwd_f32(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
-  const unsigned blocks = (unsigned)(((int64_t)s.q_len * s.group + 15) / 16);
+  const unsigned blocks = (unsigned)(((int64_t)s.q_len * s.group + 15) / 16), key_blocks = (unsigned)(((int64_t)s.kv_len + 15) / 16);
+  // One launch while every block has a CU: beyond that its registers, those of both, cost more blocks at a time than a launch does. us of backward, one
+  // launch / two: 2 x 128 rows, 96 states, 4 heads of 64 (112 blocks) 12.0 / 18.9, of 128 24.1 / 34.3; 4 x 512, 512, 8 of 64 (2048) 200 / 178; 2 x 99,
+  // 5, 20 of 128 (320) 44.8 / 28.4.
+  if ((int64_t)(blocks + key_blocks) * s.kv_heads * s.batch <= 256) {
+    hipLaunchKernelGGL((cross_bwd_f32_kernel<D>), dim3(key_blocks + blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p, (int)key_blocks);
+    return;
+  }
   hipLaunchKernelGGL((cross_dq_f32_kernel<D>), dim3(blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
-  hipLaunchKernelGGL((cross_dkdv_f32_kernel<D>), dim3((s.kv_len + 15) / 16, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
+  hipLaunchKernelGGL((cross_dkdv_f32_kernel<D>), dim3(key_blocks, s.kv_heads, s.batch), dim3(256), 0, st, s, p);
 }
 
 }  // namespace
