@@ -541,13 +541,19 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossShape sh, CrossOpe
 struct BwdParts {
   float* o;
   int splits;
+  float* off;   // of dq: [split][head][row] sums of the scores' gradients
   template <int D>
   __device__ __forceinline__ float* rows(int head, int heads, int split, int arrays, int array, int64_t n_rows, int64_t r) const {
     return o + ((((int64_t)split * heads + head) * arrays + array) * n_rows + r) * D;
   }
 };
 
-// dQ of 128 / G rows. Also leaves delta = rowsum(dO * O) of its rows, laid out as lse, for the kernel of dK and dV.
+// dQ of 128 / G rows. Also leaves delta of its rows, laid out as lse, for the kernel of dK and dV.
+// delta = rowsum(dO * O), of the stored O, whose rounding is a third of what the scores' gradients as the matrix instructions' operands (16 bits) put
+// into dQ. Where a lane has registers for it (not 128-wide heads at two wavefronts per SIMD) it is taken out again: the gradients of a row's scores add
+// up to 0, so what they do add up to is what delta lacks, and dQ gets as much of sum p K, a fourth product, less. Error of dQ, in units of what rounding
+// the result costs, and us, without / with: 8 x 512 rows, 1024 states, 16 heads of 64 1.495 / 1.444, 28.9 / 33.3; 5 x 1143, 777, 4 in IEEE half 1.504 /
+// 1.436, 14.0 / 15.5.
 template <int D, bool F16, int G>
 __global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kernel(CrossShape sh, CrossOperands p, int nx, float* __restrict__ delta, BwdParts parts) {
   constexpr int NS = D / 16, NT = D / 32, TE = Tile<D>::ELEMS, RB = 128 / G;
@@ -587,8 +593,11 @@ __global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kern
     }
   }
   my_delta += __shfl_xor(my_delta, 32, 64);
-  f32x16_t dq[NT];
+  constexpr bool EXACT = D == 64 || G == 2;
+  f32x16_t dq[NT], pk[EXACT ? NT : 1];
   zero(dq);
+  zero(pk);
+  float off = 0.f;
 
   const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
   const StateTiles<D> kt((const bf16_t*)p.k + kv0, sh.kv_stride, n_keys, lane, wave), vt((const bf16_t*)p.v + kv0, sh.kv_stride, n_keys, lane, wave);
@@ -643,45 +652,73 @@ __global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kern
       f32x16_t sc, dp;
       scores(ktile, vtile, i, kv0, sc, dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - my_delta);
+      for (int r = 0; r < 16; ++r) {
+        dp[r] = sc[r] * (dp[r] - my_delta);
+        if (EXACT) off += dp[r];
+      }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const bf16x8_t dsf = pack8<F16>(dp, half);
+        if constexpr (EXACT) {
+          const bf16x8_t pf = pack8<F16>(sc, half);   // (a correction's factor: its rounding is of no account)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) dq[t] = mfma16<F16>(frag_tr<D>(ktile, ft_base, i * 32 + 16 * half, t), dsf, dq[t]);
+          for (int t = 0; t < NT; ++t) {
+            const bf16x8_t kt = frag_tr<D>(ktile, ft_base, i * 32 + 16 * half, t);
+            dq[t] = mfma16<F16>(kt, dsf, dq[t]);
+            pk[t] = mfma16<F16>(kt, pf, pk[t]);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) dq[t] = mfma16<F16>(frag_tr<D>(ktile, ft_base, i * 32 + 16 * half, t), dsf, dq[t]);
+        }
       }
     }
   };
   tile_ring<2, G * 2 * StateTiles<D>::MINE>((n_tiles + G - 1) / G, issue_step, compute);
-  // (group 0 of the last split has the tile of a walk that is one)
-  if (grp == 0 && blk.split == parts.splits - 1 && kc == 0 && my_row < n_rows) delta[stat] = my_delta;
-  if constexpr (G > 1) {
-    constexpr int REGS = NT * 16;
+  if constexpr (EXACT) off += __shfl_xor(off, 32, 64);
+  constexpr int REGS = 2 * NT * 16 + 1;
+  if constexpr (G == 2) {
     if (grp > 0) {
       float* s = group_slot<G, REGS>(smem, grp, row_wave, lane);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[(t * 16 + r) * 64] = dq[t][r];
+        for (int r = 0; r < 16; ++r) { s[(t * 16 + r) * 64] = dq[t][r]; s[((NT + t) * 16 + r) * 64] = pk[t][r]; }
+      s[2 * NT * 16 * 64] = off;
     }
     __syncthreads();
     if (grp > 0) return;
-    for (int g = 1; g < G; ++g) {
-      const float* s = group_slot<G, REGS>(smem, g, row_wave, lane);
+    const float* s = group_slot<G, REGS>(smem, 1, row_wave, lane);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dq[t][r] += s[(t * 16 + r) * 64];
-    }
+      for (int r = 0; r < 16; ++r) { dq[t][r] += s[(t * 16 + r) * 64]; pk[t][r] += s[((NT + t) * 16 + r) * 64]; }
+    off += s[2 * NT * 16 * 64];
   }
   if (wave_row >= n_rows) return;
-  const auto value = [&](int t, int e) { return dq[t][e] * sh.scale; };
-  if (parts.splits > 1) {
-    store_part<D>(parts.rows<D>(blk.head, sh.batch * sh.kv_heads, blk.split, 1, 0, n_rows, wave_row), lane, n_rows - wave_row, value);
-    return;
+  if constexpr (G == 2) {
+    if (parts.splits > 1) {   // (the kernel that adds them up does the rest; a walk of one tile is the last split's)
+      const int heads = sh.batch * sh.kv_heads;
+      store_part<D>(parts.rows<D>(blk.head, heads, blk.split, 2, 0, n_rows, wave_row), lane, n_rows - wave_row, [&](int t, int e) { return dq[t][e]; });
+      store_part<D>(parts.rows<D>(blk.head, heads, blk.split, 2, 1, n_rows, wave_row), lane, n_rows - wave_row, [&](int t, int e) { return pk[t][e]; });
+      if (kc == 0 && my_row < n_rows) {
+        parts.off[((int64_t)blk.split * heads + blk.head) * n_rows + my_row] = off;
+        if (blk.split == parts.splits - 1) delta[stat] = my_delta;
+      }
+      return;
+    }
   }
+  if constexpr (EXACT) {
+    my_delta += off;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[t][r] = fmaf(-off, pk[t][r], dq[t][r]);
+  }
+  if (kc == 0 && my_row < n_rows) delta[stat] = my_delta;
+  const auto value = [&](int t, int e) { return dq[t][e] * sh.scale; };
   bf16_t* out = (bf16_t*)p.dq + (int64_t)b * sh.q_len * sh.q_stride + head0;
-  bf16_t* stage = smem + row_wave * (G > 1 ? NT * 16 * 128 : RowStage<D, F16>::ELEMS);
+  bf16_t* stage = smem + row_wave * (G == 2 ? REGS * 128 : RowStage<D, F16>::ELEMS);   // (a wavefront writes over its own slot of what the groups handed it)
   RowStage<D, F16>::store(stage, lane, min(32, n_rows - wave_row), value, [&](int r) { return out + rows.at(wave_row + r, sh.q_stride, D); });
 }
 
@@ -1167,12 +1204,11 @@ __global__ __launch_bounds__(256, 1) void cross_bwd_short_kernel(CrossShape sh, 
   }
 }
 
-// Adds up the parts of a gradient, in their order, eight columns per thread. QUERY: dq, rows of which are CrossRows; else dk and dv.
-template <int D, bool F16, bool QUERY>
+// Adds up the parts of dk and dv, in their order, eight columns per thread.
+template <int D, bool F16>
 __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
-  constexpr int C = D / 8, ARRAYS = QUERY ? 1 : 2;
-  const CrossRows rows(sh);
-  const int64_t n_rows = QUERY ? rows.count() : sh.kv_len, heads = (int64_t)sh.batch * sh.kv_heads, items = heads * ARRAYS * n_rows * C;
+  constexpr int C = D / 8;
+  const int64_t heads = (int64_t)sh.batch * sh.kv_heads, items = heads * 2 * sh.kv_len * C;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= items) return;
   float v[8], w[8];
@@ -1183,11 +1219,33 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOper
     for (int e = 0; e < 8; ++e) v[e] += w[e];
   }
   const int c = (int)(i % C) * 8;
-  const int64_t row = i / C, r = row % n_rows, plane = row / n_rows, head = plane / ARRAYS, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
-  bf16_t* dst;
-  if (QUERY) dst = (bf16_t*)p.dq + b * sh.q_len * sh.q_stride + h * sh.group * D + rows.at((int)r, sh.q_stride, D);
-  else dst = (bf16_t*)(plane % ARRAYS ? p.dv : p.dk) + (b * sh.kv_len + r) * sh.kv_stride + h * D;
-  store8h<F16>(dst + c, v);
+  const int64_t row = i / C, r = row % sh.kv_len, plane = row / sh.kv_len, head = plane / 2, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
+  store8h<F16>((bf16_t*)(plane % 2 ? p.dv : p.dk) + (b * sh.kv_len + r) * sh.kv_stride + h * D + c, v);
+}
+// The same of dq, whose rows are CrossRows: dq, sum p K and what delta lacks, of which it makes the one of all splits.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void cross_sum_rows_kernel(CrossShape sh, CrossOperands p, BwdParts parts, float* __restrict__ delta) {
+  constexpr int C = D / 8;
+  const CrossRows rows(sh);
+  const int64_t n_rows = rows.count(), heads = (int64_t)sh.batch * sh.kv_heads;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= heads * n_rows * C) return;
+  const int c = (int)(i % C) * 8;
+  const int64_t row = i / C, r = row % n_rows, head = row / n_rows, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
+  float dq[8] = {}, pk[8] = {}, w[8], off = 0.f;
+  for (int s = 0; s < parts.splits; ++s) {
+    load8(parts.rows<D>((int)head, (int)heads, s, 2, 0, n_rows, r) + c, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dq[e] += w[e];
+    load8(parts.rows<D>((int)head, (int)heads, s, 2, 1, n_rows, r) + c, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pk[e] += w[e];
+    off += parts.off[(s * heads + head) * n_rows + r];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) dq[e] = fmaf(-off, pk[e], dq[e]) * sh.scale;
+  if (c == 0) delta[(b * sh.heads + h * sh.group) * sh.q_len + rows.stat((int)r)] += off;
+  store8h<F16>((bf16_t*)p.dq + b * sh.q_len * sh.q_stride + h * sh.group * D + rows.at((int)r, sh.q_stride, D) + c, dq);
 }
 
 // ======================================== launches ======================================================
@@ -1199,8 +1257,8 @@ struct Form { int groups, nx, splits; };
 // groups fit one), 128-wide ones, whose two groups fill the LDS of a CU, while those of 64 rows are. us, one group / two: 64-wide, forward 2 x 512
 // rows, 1024 states, 16 heads (128 blocks of 128) 19.8 / 13.1; 5 x 1143, 777, 4 (180) 14.1 / 11.6; 8 x 512, 1024, 16 (512) 24.1 / 28.9; dQ and dK/dV of
 // the second 51.3 / 36.2, of the third 75.7 / 79.7; 128-wide, forward 1 x 1024, 1024, 20 heads (320 blocks of 64) 26.2 / 34.7, dQ and dK/dV 67 / 90.
-// Splits of the walk, which a second kernel adds up (5 to 10 us): while the blocks are far fewer than the CUs and the walk is long. 1 x 128 rows, 8192 states, 16
-// heads of 128 in 2 / 4 / 8 splits 58.9 / 37.4 / 29.7; 1 x 512, 4096, 16 of 64 (128 blocks) in 1 / 2 / 4 26.3 / 26.2 / 25.6.
+// Splits of the walk, which a second kernel adds up (5 to 10 us): while the blocks, then of two groups, are far fewer than the CUs and the walk is long.
+// 1 x 128 rows, 8192 states, 16 heads of 128 in 2 / 4 / 8 splits 58.9 / 37.4 / 29.7; 1 x 512, 4096, 16 of 64 (128 blocks) in 1 / 2 / 4 26.3 / 26.2 / 25.6.
 Form form(int head_dim, int64_t rows, int64_t walk, int64_t heads) {
   Form f;
   const int64_t tiles = (walk + 63) / 64, wide = (rows + 127) / 128 * heads, narrow = (rows + 63) / 64 * heads;
@@ -1273,7 +1331,7 @@ BwdPlan bwd_plan(int head_dim, const CrossShape& s) {
   f.q = form(head_dim, rows, s.kv_len, heads);
   f.kv = form(head_dim, s.kv_len, rows, heads);
   f.delta_bytes = up256((size_t)(heads * rows) * 4);
-  const size_t dq = f.q.splits > 1 ? (size_t)(heads * rows * f.q.splits) * head_dim * 4 : 0;
+  const size_t dq = f.q.splits > 1 ? (size_t)(heads * rows * f.q.splits) * (2 * head_dim + 1) * 4 : 0;
   const size_t dkv = f.kv.splits > 1 ? (size_t)(heads * s.kv_len * f.kv.splits) * 2 * head_dim * 4 : 0;
   f.total = f.delta_bytes + up256(dq > dkv ? dq : dkv);
   return f;
@@ -1310,7 +1368,7 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
   float *delta = p.ws, *memory = (float*)((char*)p.ws + f.delta_bytes);
   constexpr size_t tile = 2 * Tile<D>::ELEMS * sizeof(bf16_t), rows_out = (size_t)4 * RowStage<D, F16>::ELEMS * 2;
   if (f.one) {
-    const BwdParts parts = {p.ws, f.kv.splits};
+    const BwdParts parts = {p.ws, f.kv.splits, nullptr};
     static_assert(4 * 2 * D * 16 * 4 <= SHORT_BWD_LDS<D>, "dK and dV of 32 states of four wavefronts");
     const int64_t blocks = cross_grid(s, 1, f.kv.splits);
     if (s.kv_len <= 64) launch(cross_bwd_short_kernel<D, F16, 2>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
@@ -1318,23 +1376,23 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
       if (s.kv_len <= 96) launch(cross_bwd_short_kernel<D, F16, 3>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
       else launch(cross_bwd_short_kernel<D, F16, 4>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
     }
-    if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16, false>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
+    if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
     return;
   }
   {
-    const BwdParts parts = {memory, f.q.splits};
+    const BwdParts parts = {memory, f.q.splits, memory + heads * rows * f.q.splits * 2 * D};
     const int64_t blocks = cross_grid(s, f.q.nx, f.q.splits);
     if (f.q.groups == 2) launch(cross_dq_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.q.nx, delta, parts);
     else launch(cross_dq_kernel<D, F16, 1>, blocks, std::max(2 * tile, rows_out), st, s, p, f.q.nx, delta, parts);
-    if (f.q.splits > 1) launch(cross_sum_kernel<D, F16, true>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts);
+    if (f.q.splits > 1) launch(cross_sum_rows_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts, delta);
   }
   {
-    const BwdParts parts = {memory, f.kv.splits};
+    const BwdParts parts = {memory, f.kv.splits, nullptr};
     const int64_t blocks = cross_grid(s, f.kv.nx, f.kv.splits);
     constexpr size_t stage = tile + 512, meet = (size_t)2 * D * 2 * 64 * sizeof(float);   // two wavefronts' dK and dV
     if (f.kv.groups == 2) launch(cross_dkdv_kernel<D, F16, 2>, blocks, std::max(4 * stage, meet), st, s, p, f.kv.nx, (const float*)delta, parts);
     else launch(cross_dkdv_kernel<D, F16, 1>, blocks, std::max(2 * stage, rows_out), st, s, p, f.kv.nx, (const float*)delta, parts);
-    if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16, false>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
+    if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
   }
 }
 
