@@ -1256,7 +1256,7 @@ struct Form { int groups, nx, splits; };
 // Two groups, i.e. blocks of 64 rows that take two tiles at a time: 64-wide heads while blocks of 128 rows are at most one per CU (two of those with two
 // groups fit one), 128-wide ones, whose two groups fill the LDS of a CU, while those of 64 rows are. us, one group / two: 64-wide, forward 2 x 512
 // rows, 1024 states, 16 heads (128 blocks of 128) 19.8 / 13.1; 5 x 1143, 777, 4 (180) 14.1 / 11.6; 8 x 512, 1024, 16 (512) 24.1 / 28.9; dQ and dK/dV of
-// the second 51.3 / 36.2, of the third 75.7 / 79.7; 128-wide, forward 1 x 1024, 1024, 20 heads (320 blocks of 64) 26.2 / 34.7, dQ and dK/dV 67 / 90.
+// the second 51.1 / 46.3, of the third 75.6 / 84.0; 128-wide, forward 1 x 1024, 1024, 20 heads (320 blocks of 64) 26.2 / 34.7, dQ and dK/dV 68 / 108.
 // Splits of the walk, which a second kernel adds up (5 to 10 us): while the blocks, then of two groups, are far fewer than the CUs and the walk is long.
 // 1 x 128 rows, 8192 states, 16 heads of 128 in 2 / 4 / 8 splits 58.9 / 37.4 / 29.7; 1 x 512, 4096, 16 of 64 (128 blocks) in 1 / 2 / 4 26.3 / 26.2 / 25.6.
 Form form(int head_dim, int64_t rows, int64_t walk, int64_t heads) {
