@@ -28,6 +28,7 @@ CASES = [   # rows, heads, head width, pairs of each axis, per axis, base
     (1, 1, 8, (4,), False, 10000.0), (1, 40, 128, (16, 24, 24), False, 10000.0), (577, 16, 64, (16, 16), True, 10000.0),
     (300, 3, 72, (12, 12, 12), True, 100.0), (65, 5, 80, (7, 0, 11, 3), False, 500000.0), (33, 2, 256, (128,), False, 1.5), (4100, 2, 16, (3, 2), True, 10000.0),
     (17, 300, 8, (1, 1), False, 10000.0), (5, 1, 64, (0, 0), True, 10.0),
+    (5003, 3, 64, (10, 12, 8), False, 10000.0), (40007, 1, 8, (2, 1), True, 100.0), (2049, 9, 72, (36,), False, 10000.0),   # rows side by side in a block
 ]
 
 
