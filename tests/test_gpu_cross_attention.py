@@ -23,7 +23,7 @@ def view(a, dtype, stride, gap=np.nan):
 
 
 class Problem:
-    def __init__(self, batch, q_len, kv_len, heads, kv_heads, width, dtype=W.BF16, lens=None, scale=0.0, strided=False, big=1.0, seed=0, poison=True):
+    def __init__(self, batch, q_len, kv_len, heads, kv_heads, width, dtype=W.BF16, lens=None, scale=0.0, strided=False, big=1.0, seed=0, poison=True, steps=False):
         rng = np.random.default_rng(seed + q_len * 1000 + kv_len)
         self.__dict__.update(batch=batch, q_len=q_len, kv_len=kv_len, heads=heads, kv_heads=kv_heads, width=width, dtype=dtype)
         w, kw = heads * width, kv_heads * width
@@ -35,6 +35,8 @@ class Problem:
         self.scale = scale or None
         q, k, v, do = (store(rng.standard_normal(s), dtype) for s in ((batch, q_len, w), (batch, kv_len, kw), (batch, kv_len, kw), (batch, q_len, w)))
         q = store(q * big, dtype)
+        if steps:   # values that differ in their last bit
+            v = store(1.0 + 2 * ROUND[dtype] * (v > 0), dtype)
         if self.lens is not None and poison:   # what lies behind the visible states reaches nothing
             for b, n in enumerate(np.clip(self.lens, 0, kv_len)):
                 k[b, n:], v[b, n:] = (np.nan, np.inf) if b % 2 else (-np.inf, np.nan)
@@ -121,6 +123,31 @@ def test_every_length_around_a_tile(dtype):
 def test_lengths_inside_a_group_of_states_with_blocks_for_every_unit(shape, dtype):
     """Enough blocks of the widest kind: the states end inside a wavefront's 32, and rows inside the last tile."""
     Problem(*shape, dtype=dtype, lens=[shape[2] - 47, 513, 500]).check()
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("shape", [(2, 130, 777, 4, 2, 64), (1, 64, 5000, 1, 1, 64), (3, 700, 800, 16, 16, 64), (1, 100, 700, 2, 2, 128),
+                                   (1, 40, 4000, 2, 1, 128), (2, 33, 150, 1, 1, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_where_values_differ_by_less_than_the_rounding_of_their_mean(shape, dtype):
+    """dp - delta is then no larger than what the stored out is off by, which without a correction puts R = 1.3 to 5.5 times dq into dq.
+
+    In the 2-norm, roundings being independent, relative to dq: u for the result, u (1 + R) for the gradients of the scores that are rounded in
+    front of the correction, u R for the correction's factor. 32 bits: dp and delta are sums of `width` values and of size sqrt(width), off by no more than
+    sqrt(width) 2^-24 of that, 8e-6, four times over with the probabilities and their sums, where dp - delta is about half of sqrt(width) 2 u, 8 u, and its
+    correction R of that."""
+    p = Problem(*shape, dtype=dtype, lens=[shape[2], 2 * shape[2] // 3], steps=True)
+    p.check()
+    q, k, v, do = p.host
+    u = ROUND[dtype]
+    want, out = O.cross_backward(q, k, v, do, p.lens)[0], O.cross_forward(q, k, v, p.lens)
+    s, kk, _ = O._scores(q, k, v, p.lens, shape[5] ** -0.5)
+    mean = (np.exp(s - out[1][..., None]) @ kk).transpose(0, 2, 1, 3) * shape[5] ** -0.5
+    stored = (do * (store(out[0].astype(np.float32), dtype) - out[0])).sum(-1, keepdims=True) * mean
+    norm = np.linalg.norm(want)
+    times = np.linalg.norm(stored) / norm
+    limit = u * (2 + 2 * times) + (1 + times) * 4 * 8e-6 / (8 * u)
+    assert times > 1 and times > 10 * limit    # (else this says nothing)
+    assert np.linalg.norm(p.heads_of(p.dq) - want) <= limit * norm
 
 
 @pytest.mark.parametrize("width", [64, 128])
