@@ -1204,6 +1204,222 @@ __global__ __launch_bounds__(256, 1) void cross_bwd_short_kernel(CrossShape sh, 
   }
 }
 
+// ================================ backward: at most 32 rows of a head ===================================
+// As in forward, every wavefront walks tiles of 32 states of its own. All rows are in one tile, so dK and dV of a tile's states are complete at once,
+// and only dQ is a sum over the walk: K and V are read once, for all gradients. The products want the scores either way round, S^T = K Q^T for dQ and
+// S = Q K^T for dK and dV, and both are computed (seven products), which spares a way through LDS. delta as in cross_dq_kernel: of the stored O, and
+// corrected in dQ. Bound by memory where the walk is long. us, against two kernels on tiles: 16 x 4 rows, 16384 states, 8 key heads of 128 432 / 828
+// (2.15 GB, 5.0 TB/s); 16 x 8, 4096, 16 of 64 128 / 198; 32 x 32, 500, 16 of 128 75.6 / 119, of 64 43.2 / 54.7; 7 x 2, 242, 2 of 64 9.1 / 11.8; but
+// 1 x 30, 7749, 4 of 64 29.4 / 28.1.
+template <int D> constexpr int FEW_BWD_WAVES = D == 64 ? 8 : 4;
+template <int D> constexpr size_t FEW_BWD_LDS = (2 + 2 * FEW_BWD_WAVES<D>) * 32 * D * sizeof(bf16_t) + (64 + 32 * FEW_BWD_WAVES<D>) * sizeof(float);
+template <int D, bool F16>
+__global__ __launch_bounds__(64 * FEW_BWD_WAVES<D>) void cross_bwd_few_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
+  constexpr int NS = D / 16, NT = D / 32, TE = 32 * D, WAVES = FEW_BWD_WAVES<D>, SPR = D / 8, LOADS = SPR / 2;
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];   // Q, dO; per wavefront K and V, then what goes out; lse and delta; sums of scores' gradients
+  const CrossBlock blk = cross_block<true>(1, parts.splits, sh, p.lens);
+  if (blk.none) return;
+  const int b = blk.b, h = blk.h;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kc = lane >> 5;
+  const int fr_base = rows_base<D>(lane), ft_base = tr_base<D>(lane);
+  const CrossRows rows(sh);
+  const int n_rows = rows.count(), n_keys = visible(sh, p.lens, b), all_tiles = (sh.kv_len + 31) / 32;
+  const int first = split_begin(all_tiles, blk.split, parts.splits) + wave, end = split_begin(all_tiles, blk.split + 1, parts.splits);
+  const int my_row = lane & 31, ld_row = min(my_row, n_rows - 1);
+  const int64_t head0 = (int64_t)h * sh.group * D, stat = ((int64_t)b * sh.heads + h * sh.group) * sh.q_len + rows.stat(ld_row);
+  const float sl2 = LOG2E * sh.scale;
+
+  bf16_t *qtile = smem, *dtile = smem + TE, *ktile = smem + (2 + 2 * wave) * TE, *vtile = ktile + TE;
+  float *stats = reinterpret_cast<float*>(smem + (2 + 2 * WAVES) * TE), *offs = stats + 64;
+  const int64_t kv0 = (int64_t)b * sh.kv_len * sh.kv_stride + h * D;
+  const bf16_t *k = (const bf16_t*)p.k + kv0, *v = (const bf16_t*)p.v + kv0;
+  const unsigned bytes = n_keys > 0 ? (unsigned)(((int64_t)(n_keys - 1) * sh.kv_stride + D) * 2) : 0u, step = (unsigned)(32 * sh.kv_stride * 2);
+  unsigned voff[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int slot = i * 64 + lane, row = slot / SPR, pos = slot % SPR;
+    voff[i] = (unsigned)(row * sh.kv_stride * 2) + (unsigned)(pos ^ Tile<D>::f(row)) * 16u;
+  }
+  auto issue = [&](int t) {   // (hidden tiles: nothing is read)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wavefront has read of its room has arrived
+    const unsigned at = (unsigned)t * step;
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) {
+      buffer_load_lds_16_untracked(k, bytes, ktile + n * 512, voff[n] + at, 0);
+      buffer_load_lds_16_untracked(v, bytes, vtile + n * 512, voff[n] + at, 0);
+    }
+  };
+  const bool whole = n_keys <= 64, mine = first < end && 32 * first < n_keys;
+  if (!whole && mine) issue(first);
+  const bf16_t *q = (const bf16_t*)p.q + (int64_t)b * sh.q_len * sh.q_stride + head0, *dout = (const bf16_t*)p.dout + (int64_t)b * sh.q_len * sh.out_stride + head0;
+  if (wave == 0) RowTiles<D>(rows, q, sh.q_stride, lane).issue(qtile, 0);
+  if (wave == 1) RowTiles<D>(rows, dout, sh.out_stride, lane).issue(dtile, 0);
+  const float lse2 = p.lse[stat] * LOG2E;
+  float delta = 0.f;
+  {
+    const bf16_t *o = (const bf16_t*)p.out + (int64_t)b * sh.q_len * sh.out_stride + head0;
+    const int64_t at = rows.at(ld_row, sh.out_stride, D) + 8 * kc;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      float ov[8], dv[8];
+      load8h<F16>(o + at + 16 * s, ov);
+      load8h<F16>(dout + at + 16 * s, dv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(ov[e], dv[e], delta);
+    }
+    delta += __shfl_xor(delta, 32, 64);
+  }
+  // probabilities and their gradients, S^T
+  f32x16_t pr, dp;
+  auto scores = [&](int t) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) pr[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      pr = mfma16<F16>(frag_rows<D>(ktile, fr_base, 0, s), frag_rows<D>(qtile, fr_base, 0, s), pr);
+      dp = mfma16<F16>(frag_rows<D>(vtile, fr_base, 0, s), frag_rows<D>(dtile, fr_base, 0, s), dp);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      pr[r] = __builtin_amdgcn_exp2f(fmaf(pr[r], sl2, -lse2));
+      pr[r] = 32 * t + acc_row(r, lane) < n_keys ? pr[r] : 0.f;
+    }
+  };
+  wait_loads_and_lds<0>();
+  __syncthreads();
+  if (whole) {   // delta as sum p dP, which every wavefront takes: with few states that shows in dk too (see cross_dq_kernel)
+    delta = 0.f;
+#pragma unroll 1
+    for (int t = 0; 32 * t < n_keys; ++t) {
+      issue(t);
+      wait_loads_and_lds<0>();
+      asm volatile("" ::: "memory");
+      scores(t);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) delta = fmaf(pr[r], dp[r], delta);
+    }
+    delta += __shfl_xor(delta, 32, 64);
+    if (mine) issue(first);
+  }
+  if (wave == 0 && kc == 0) {   // (rows that are not there: zeros, and a p of 0)
+    stats[my_row] = my_row < n_rows ? lse2 : INFINITY;
+    stats[32 + my_row] = delta;
+  }
+  __syncthreads();
+
+  f32x16_t dq[NT], pk[NT];
+  zero(dq);
+  zero(pk);
+  float off = 0.f;
+  for (int t = first; t < end; t += WAVES) {
+    const int left = sh.kv_len - 32 * t;
+    const bool seen = 32 * t + my_row < n_keys;
+    const int64_t at = kv0 + (int64_t)32 * t * sh.kv_stride;
+    f32x16_t acc[NT];
+    const auto put = [&](void* out, float scale) {
+      RowStage<D, F16>::store(ktile, lane, min(32, left), [&](int c, int e) { return seen ? acc[c][e] * scale : 0.f; },
+                              [&](int r) { return (bf16_t*)out + at + r * sh.kv_stride; });
+    };
+    if (32 * t >= n_keys) {
+      zero(acc);
+      put(p.dk, 0.f);
+      put(p.dv, 0.f);
+      continue;
+    }
+    wait_loads_and_lds<0>();
+    asm volatile("" ::: "memory");
+    scores(t);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dp[r] = pr[r] * (dp[r] - delta);
+      off += dp[r];
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8_t pf = pack8<F16>(pr, half), dsf = pack8<F16>(dp, half);
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const bf16x8_t kt = frag_tr<D>(ktile, ft_base, 16 * half, c);
+        dq[c] = mfma16<F16>(kt, dsf, dq[c]);
+        pk[c] = mfma16<F16>(kt, pf, pk[c]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) pr[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      pr = mfma16<F16>(frag_rows<D>(qtile, fr_base, 0, s), frag_rows<D>(ktile, fr_base, 0, s), pr);
+      dp = mfma16<F16>(frag_rows<D>(dtile, fr_base, 0, s), frag_rows<D>(vtile, fr_base, 0, s), dp);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float4 l4 = *reinterpret_cast<const float4*>(stats + g * 8 + 4 * kc), d4 = *reinterpret_cast<const float4*>(stats + 32 + g * 8 + 4 * kc);
+      const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * g + e;
+        pr[r] = __builtin_amdgcn_exp2f(fmaf(pr[r], sl2, -ls[e]));
+        dp[r] = pr[r] * (dp[r] - ds[e]);
+      }
+    }
+    const bf16x8_t pf[2] = {pack8<F16>(pr, 0), pack8<F16>(pr, 1)}, dsf[2] = {pack8<F16>(dp, 0), pack8<F16>(dp, 1)};
+    zero(acc);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int c = 0; c < NT; ++c) acc[c] = mfma16<F16>(frag_tr<D>(dtile, ft_base, 16 * half, c), pf[half], acc[c]);
+    put(p.dv, 1.f);
+    zero(acc);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int c = 0; c < NT; ++c) acc[c] = mfma16<F16>(frag_tr<D>(qtile, ft_base, 16 * half, c), dsf[half], acc[c]);
+    put(p.dk, sh.scale);
+    if (t + WAVES < end && 32 * (t + WAVES) < n_keys) issue(t + WAVES);
+  }
+  // every wavefront puts some of the accumulators of all together: registers REGS w .. of the 16 NT, dq's, then those of sum p K
+  constexpr int REGS = 16 * NT / WAVES;
+  static_assert(REGS % 2 == 0 && 16 % REGS == 0, "whole pairs of columns, of one 32-column block");
+  float* slots = reinterpret_cast<float*>(smem + 2 * TE) + lane;
+  off += __shfl_xor(off, 32, 64);
+  if (kc == 0) offs[wave * 32 + my_row] = off;
+  float sum[2][REGS];
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) slots[((wave * NT + t) * 16 + r) * 64] = a ? pk[t][r] : dq[t][r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) sum[a][r] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+#pragma unroll
+      for (int r = 0; r < REGS; ++r) sum[a][r] += slots[(w * NT * 16 + wave * REGS + r) * 64];
+  }
+  if (my_row >= n_rows) return;
+  off = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) off += offs[w * 32 + my_row];
+  const int reg = wave * REGS % 16, col = wave * REGS / 16 * 32 + 8 * (reg / 4) + 4 * kc + reg % 4;   // of the first of them
+  bf16_t* out = (bf16_t*)p.dq + (int64_t)b * sh.q_len * sh.q_stride + head0 + rows.at(my_row, sh.q_stride, D) + col;
+  const int heads = sh.batch * sh.kv_heads;
+#pragma unroll
+  for (int r = 0; r < REGS; r += 2) {   // (registers 4 g .. 4 g + 3: consecutive columns; the next four eight columns on)
+    const int c = r / 4 * 8 + r % 4;
+    if (parts.splits > 1) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+        *reinterpret_cast<float2*>(parts.rows<D>(blk.head, heads, blk.split, 2, a, n_rows, my_row) + col + c) = make_float2(sum[a][r], sum[a][r + 1]);
+    } else {
+      *reinterpret_cast<uint32_t*>(out + c) = pack2<F16>(fmaf(-off, sum[1][r], sum[0][r]) * sh.scale, fmaf(-off, sum[1][r + 1], sum[0][r + 1]) * sh.scale);
+    }
+  }
+  if (parts.splits > 1 && wave == 0 && kc == 0) parts.off[((int64_t)blk.split * heads + blk.head) * n_rows + my_row] = off;
+}
+
 // Adds up the parts of dk and dv, in their order, eight columns per thread.
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOperands p, BwdParts parts) {
@@ -1213,6 +1429,7 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOper
   if (i >= items) return;
   float v[8], w[8];
   load8(parts.o + 8 * i, v);
+#pragma unroll 4
   for (int s = 1; s < parts.splits; ++s) {
     load8(parts.o + 8 * (i + s * items), w);
 #pragma unroll
@@ -1222,7 +1439,7 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOper
   const int64_t row = i / C, r = row % sh.kv_len, plane = row / sh.kv_len, head = plane / 2, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
   store8h<F16>((bf16_t*)(plane % 2 ? p.dv : p.dk) + (b * sh.kv_len + r) * sh.kv_stride + h * D + c, v);
 }
-// The same of dq, whose rows are CrossRows: dq, sum p K and what delta lacks, of which it makes the one of all splits.
+// The same of dq, whose rows are CrossRows: dq, sum p K and what delta lacks, of which it makes the one of all splits (delta may be NULL: nobody wants it).
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void cross_sum_rows_kernel(CrossShape sh, CrossOperands p, BwdParts parts, float* __restrict__ delta) {
   constexpr int C = D / 8;
@@ -1233,6 +1450,7 @@ __global__ __launch_bounds__(256) void cross_sum_rows_kernel(CrossShape sh, Cros
   const int c = (int)(i % C) * 8;
   const int64_t row = i / C, r = row % n_rows, head = row / n_rows, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
   float dq[8] = {}, pk[8] = {}, w[8], off = 0.f;
+#pragma unroll 4
   for (int s = 0; s < parts.splits; ++s) {
     load8(parts.rows<D>((int)head, (int)heads, s, 2, 0, n_rows, r) + c, w);
 #pragma unroll
@@ -1244,7 +1462,7 @@ __global__ __launch_bounds__(256) void cross_sum_rows_kernel(CrossShape sh, Cros
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) dq[e] = fmaf(-off, pk[e], dq[e]) * sh.scale;
-  if (c == 0) delta[(b * sh.heads + h * sh.group) * sh.q_len + rows.stat((int)r)] += off;
+  if (delta && c == 0) delta[(b * sh.heads + h * sh.group) * sh.q_len + rows.stat((int)r)] += off;
   store8h<F16>((bf16_t*)p.dq + b * sh.q_len * sh.q_stride + h * sh.group * D + rows.at((int)r, sh.q_stride, D) + c, dq);
 }
 
@@ -1286,6 +1504,18 @@ int few_splits(int head_dim, int64_t walk, int64_t heads) {
   }
   return best;
 }
+// The same for backward, in us: 4 for a block's beginning and end, 3 for a tile.
+int few_bwd_splits(int head_dim, int64_t walk, int64_t heads) {
+  const int64_t tiles = (walk + 31) / 32, waves = head_dim == 64 ? 8 : 4;
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= MAX_SPLITS && (s == 1 || tiles >= waves * s); ++s) {
+    const int64_t blocks = heads * s, rounds = (blocks + 255) / 256, steps = (tiles + waves * s - 1) / (waves * s);
+    const double t = rounds * (4.0 + steps * 3.0) + (s > 1 ? 5.0 : 0.0);
+    if (t < least) { least = t; best = s; }
+  }
+  return best;
+}
 // Blocks that share the rows of a head (cross_bwd_short_kernel), one at a time on each CU. Estimated in us: 5 for a block's beginning and end, 2.5
 // for 128 rows, 5 for the kernel that adds up the blocks' parts.
 int short_splits(int64_t rows, int64_t heads) {
@@ -1317,15 +1547,23 @@ FwdPlan fwd_plan(int head_dim, const CrossShape& s) {
   f.total = f.form.splits > 1 ? f.o_bytes + up256(all * 4) : 0;
   return f;
 }
-struct BwdPlan { bool one; Form q, kv; size_t delta_bytes, total; };   // the parts of dq and those of dk and dv share memory one after the other
+struct BwdPlan { bool one, few; Form q, kv; size_t delta_bytes, total; };   // the parts of dq and those of dk and dv share memory one after the other
 BwdPlan bwd_plan(int head_dim, const CrossShape& s) {
   BwdPlan f;
   const int64_t rows = (int64_t)s.q_len * s.group, heads = (int64_t)s.batch * s.kv_heads;
   f.one = s.kv_len <= (head_dim == 64 ? SHORT_BWD_KEYS<64> : SHORT_BWD_KEYS<128>);
   if (f.one) {
+    f.few = false;
     f.q = f.kv = Form{1, 1, short_splits(rows, heads)};
     f.delta_bytes = 0;
     f.total = f.kv.splits > 1 ? up256((size_t)(heads * s.kv_len * f.kv.splits) * 2 * head_dim * 4) : 256;   // (never 0: one is always passed)
+    return f;
+  }
+  f.few = rows <= FEW_ROWS;
+  if (f.few) {
+    f.q = f.kv = Form{1, 1, few_bwd_splits(head_dim, s.kv_len, heads)};
+    f.delta_bytes = 0;
+    f.total = f.q.splits > 1 ? up256((size_t)(heads * rows * f.q.splits) * (2 * head_dim + 1) * 4) : 256;
     return f;
   }
   f.q = form(head_dim, rows, s.kv_len, heads);
@@ -1377,6 +1615,13 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
       else launch(cross_bwd_short_kernel<D, F16, 4>, blocks, SHORT_BWD_LDS<D>, st, s, p, parts);
     }
     if (f.kv.splits > 1) launch(cross_sum_kernel<D, F16>, (heads * s.kv_len * 2 * (D / 8) + 255) / 256, 0, st, s, p, parts);
+    return;
+  }
+  if (f.few) {
+    const BwdParts parts = {p.ws, f.q.splits, p.ws + heads * rows * f.q.splits * 2 * D};
+    static_assert(RowStage<D, F16>::ELEMS <= 2 * 32 * D, "32 rows on their way out in the room of K and V");
+    launch<64 * FEW_BWD_WAVES<D>>(cross_bwd_few_kernel<D, F16>, cross_grid(s, 1, f.q.splits), FEW_BWD_LDS<D>, st, s, p, parts);
+    if (f.q.splits > 1) launch(cross_sum_rows_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts, (float*)nullptr);
     return;
   }
   {

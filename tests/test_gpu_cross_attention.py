@@ -126,8 +126,16 @@ def test_lengths_inside_a_group_of_states_with_blocks_for_every_unit(shape, dtyp
 
 
 @pytest.mark.parametrize("dtype", [W.BF16, W.FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("shape", [(9, 32, 1500, 1, 1, 64), (9, 3, 1500, 8, 1, 128), (9, 1, 140, 40, 40, 128), (9, 7, 161, 8, 2, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_few_rows(shape, dtype):
+    """Lengths around the tiles of 32 states, of one and two tiles (which take delta another way), and whole tiles that are hidden."""
+    kv = shape[2]
+    Problem(*shape, dtype=dtype, lens=[1, 0, 31, 32, 33, 64, 65, kv - 1, kv - 33], strided=True).check()
+
+
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16], ids=["bf16", "fp16"])
 @pytest.mark.parametrize("shape", [(2, 130, 777, 4, 2, 64), (1, 64, 5000, 1, 1, 64), (3, 700, 800, 16, 16, 64), (1, 100, 700, 2, 2, 128),
-                                   (1, 40, 4000, 2, 1, 128), (2, 33, 150, 1, 1, 64)], ids=lambda s: "x".join(map(str, s)))
+                                   (1, 40, 4000, 2, 1, 128), (2, 33, 150, 1, 1, 64), (2, 16, 3000, 2, 1, 64), (2, 8, 999, 2, 2, 128)], ids=lambda s: "x".join(map(str, s)))
 def test_gradients_where_values_differ_by_less_than_the_rounding_of_their_mean(shape, dtype):
     """dp - delta is then no larger than what the stored out is off by, which without a correction puts R = 1.3 to 5.5 times dq into dq.
 
