@@ -1209,8 +1209,7 @@ __global__ __launch_bounds__(256, 1) void cross_bwd_short_kernel(CrossShape sh, 
 // and only dQ is a sum over the walk: K and V are read once, for all gradients. The products want the scores either way round, S^T = K Q^T for dQ and
 // S = Q K^T for dK and dV, and both are computed (seven products), which spares a way through LDS. delta as in cross_dq_kernel: of the stored O, and
 // corrected in dQ. Bound by memory where the walk is long. us, against two kernels on tiles: 16 x 4 rows, 16384 states, 8 key heads of 128 432 / 828
-// (2.15 GB, 5.0 TB/s); 16 x 8, 4096, 16 of 64 128 / 198; 32 x 32, 500, 16 of 128 75.6 / 119, of 64 43.2 / 54.7; 7 x 2, 242, 2 of 64 9.1 / 11.8; but
-// 1 x 30, 7749, 4 of 64 29.4 / 28.1.
+// (2.15 GB, 5.0 TB/s); 16 x 8, 4096, 16 of 64 128 / 198; 32 x 32, 500, 16 of 128 75.6 / 119, of 64 43.2 / 54.7; 7 x 2, 242, 2 of 64 9.1 / 11.8.
 template <int D> constexpr int FEW_BWD_WAVES = D == 64 ? 8 : 4;
 template <int D> constexpr size_t FEW_BWD_LDS = (2 + 2 * FEW_BWD_WAVES<D>) * 32 * D * sizeof(bf16_t) + (64 + 32 * FEW_BWD_WAVES<D>) * sizeof(float);
 template <int D, bool F16>
@@ -1440,18 +1439,19 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(CrossShape sh, CrossOper
   store8h<F16>((bf16_t*)(plane % 2 ? p.dv : p.dk) + (b * sh.kv_len + r) * sh.kv_stride + h * D + c, v);
 }
 // The same of dq, whose rows are CrossRows: dq, sum p K and what delta lacks, of which it makes the one of all splits (delta may be NULL: nobody wants it).
+// A wavefront takes a row, its lanes eight columns each and the splits between them: a thread alone took 13 us for 30 splits, not 4.2.
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void cross_sum_rows_kernel(CrossShape sh, CrossOperands p, BwdParts parts, float* __restrict__ delta) {
-  constexpr int C = D / 8;
+  constexpr int C = D / 8, GROUPS = 64 / C;
   const CrossRows rows(sh);
   const int64_t n_rows = rows.count(), heads = (int64_t)sh.batch * sh.kv_heads;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= heads * n_rows * C) return;
-  const int c = (int)(i % C) * 8;
-  const int64_t row = i / C, r = row % n_rows, head = row / n_rows, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= heads * n_rows) return;
+  const int lane = threadIdx.x & 63, c = lane % C * 8, g = lane / C;
+  const int64_t r = row % n_rows, head = row / n_rows, b = head / sh.kv_heads, h = head - b * sh.kv_heads;
   float dq[8] = {}, pk[8] = {}, w[8], off = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < parts.splits; ++s) {
+#pragma unroll 2
+  for (int s = g; s < parts.splits; s += GROUPS) {
     load8(parts.rows<D>((int)head, (int)heads, s, 2, 0, n_rows, r) + c, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dq[e] += w[e];
@@ -1460,6 +1460,13 @@ __global__ __launch_bounds__(256) void cross_sum_rows_kernel(CrossShape sh, Cros
     for (int e = 0; e < 8; ++e) pk[e] += w[e];
     off += parts.off[(s * heads + head) * n_rows + r];
   }
+#pragma unroll
+  for (int o = C; o < 64; o *= 2) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { dq[e] += __shfl_xor(dq[e], o, 64); pk[e] += __shfl_xor(pk[e], o, 64); }
+    off += __shfl_xor(off, o, 64);
+  }
+  if (g != 0) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) dq[e] = fmaf(-off, pk[e], dq[e]) * sh.scale;
   if (delta && c == 0) delta[(b * sh.heads + h * sh.group) * sh.q_len + rows.stat((int)r)] += off;
@@ -1621,7 +1628,7 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
     const BwdParts parts = {p.ws, f.q.splits, p.ws + heads * rows * f.q.splits * 2 * D};
     static_assert(RowStage<D, F16>::ELEMS <= 2 * 32 * D, "32 rows on their way out in the room of K and V");
     launch<64 * FEW_BWD_WAVES<D>>(cross_bwd_few_kernel<D, F16>, cross_grid(s, 1, f.q.splits), FEW_BWD_LDS<D>, st, s, p, parts);
-    if (f.q.splits > 1) launch(cross_sum_rows_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts, (float*)nullptr);
+    if (f.q.splits > 1) launch(cross_sum_rows_kernel<D, F16>, (heads * rows + 3) / 4, 0, st, s, p, parts, (float*)nullptr);
     return;
   }
   {
@@ -1629,7 +1636,7 @@ void bwd(const CrossShape& s, const CrossOperands& p, hipStream_t st) {
     const int64_t blocks = cross_grid(s, f.q.nx, f.q.splits);
     if (f.q.groups == 2) launch(cross_dq_kernel<D, F16, 2>, blocks, 4 * tile, st, s, p, f.q.nx, delta, parts);
     else launch(cross_dq_kernel<D, F16, 1>, blocks, std::max(2 * tile, rows_out), st, s, p, f.q.nx, delta, parts);
-    if (f.q.splits > 1) launch(cross_sum_rows_kernel<D, F16>, (heads * rows * (D / 8) + 255) / 256, 0, st, s, p, parts, delta);
+    if (f.q.splits > 1) launch(cross_sum_rows_kernel<D, F16>, (heads * rows + 3) / 4, 0, st, s, p, parts, delta);
   }
   {
     const BwdParts parts = {memory, f.kv.splits, nullptr};
