@@ -200,7 +200,7 @@ __device__ __forceinline__ void dq_f32(const CrossShape& sh, const CrossOperands
       const f32x4_t s = rows_times_rows<D>(kf, qf), dp = rows_times_rows<D>(vf, df);
       f32x4_t ds;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ds[r] = 16 * t + 4 * g + r < n ? __expf(s[r] * sh.scale - lse) * (dp[r] - my_delta) : 0.f;
+      for (int r = 0; r < 4; ++r) ds[r] = 16 * t + 4 * g + r < n ? __expf(s[r] * sh.scale - lse) * (dp[r] - (n_keys == 1 ? dp[r] : my_delta)) : 0.f;   // (a state alone: exactly 0)
       *reinterpret_cast<f32x4_t*>(grad + i * PITCH + 16 * t + 4 * g) = ds;
     }
     __syncthreads();
@@ -262,7 +262,7 @@ __device__ __forceinline__ void dkdv_f32(const CrossShape& sh, const CrossOperan
         const int64_t stat = stats + rows.stat(min(r0 + mine, n_rows - 1));
         const float e = seen && mine < n ? __expf(s[r] * sh.scale - p.lse[stat]) : 0.f;
         pv[r] = e;
-        const float delta = OWN ? __shfl(row_delta, 4 * g + r, 64) : p.ws[stat];
+        const float delta = n_keys == 1 ? dp[r] : OWN ? __shfl(row_delta, 4 * g + r, 64) : p.ws[stat];
         ds[r] = seen && mine < n ? e * (dp[r] - delta) : 0.f;
       }
       *reinterpret_cast<f32x4_t*>(prob + i * PITCH + 16 * t + 4 * g) = pv;

@@ -638,14 +638,17 @@ __global__ __launch_bounds__(256, D == 128 && G == 1 ? 2 : 1) void cross_dq_kern
       // All states of the sample are here: delta as sum p dP, without the rounding of O. With few states the gradient of a score is a
       // small difference (none at all with one), where that rounding would show.
       my_delta = 0.f;
+      float only;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         f32x16_t sc, dp;
         scores(ktile, vtile, i, kv0, sc, dp);
 #pragma unroll
         for (int r = 0; r < 16; ++r) my_delta = fmaf(sc[r], dp[r], my_delta);
+        if (i == 0) only = dp[0];
       }
       my_delta += __shfl_xor(my_delta, 32, 64);
+      if (n_keys == 1) my_delta = __shfl(only, lane & 31, 64);   // p is 1, and the gradient of its score 0, exactly
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -1121,6 +1124,7 @@ __global__ __launch_bounds__(256, 1) void cross_bwd_short_kernel(CrossShape sh, 
       }
     }
     delta += __shfl_xor(delta, 32, 64);
+    if (n_keys == 1) delta = __shfl(dp[0][0], lane & 31, 64);   // (see cross_dq_kernel)
     f32x16_t dq[NT];
     zero(dq);
     __builtin_amdgcn_sched_barrier(0);
@@ -1298,6 +1302,7 @@ __global__ __launch_bounds__(64 * FEW_BWD_WAVES<D>) void cross_bwd_few_kernel(Cr
       for (int r = 0; r < 16; ++r) delta = fmaf(pr[r], dp[r], delta);
     }
     delta += __shfl_xor(delta, 32, 64);
+    if (n_keys == 1) delta = __shfl(dp[0], lane & 31, 64);   // (see cross_dq_kernel)
     if (mine) issue(first);
   }
   if (wave == 0 && kc == 0) {   // (rows that are not there: zeros, and a p of 0)

@@ -125,6 +125,19 @@ def test_lengths_inside_a_group_of_states_with_blocks_for_every_unit(shape, dtyp
     Problem(*shape, dtype=dtype, lens=[shape[2] - 47, 513, 500]).check()
 
 
+@pytest.mark.parametrize("dtype", [W.BF16, W.FP16, W.FP32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("shape", [(3, 200, 1, 4, 2, 64), (3, 40, 1, 2, 2, 128), (3, 4, 300, 4, 2, 64), (3, 4, 300, 2, 2, 128), (3, 100, 300, 4, 2, 64), (3, 100, 90, 2, 2, 128),
+                                   (3, 600, 300, 48, 48, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_a_state_alone_has_gradients_of_zero(shape, dtype):
+    """Its probability is 1 whatever its score."""
+    p = Problem(*shape, dtype=dtype, lens=[1, shape[2], 1])
+    p.forward()
+    p.backward()
+    for b in range(shape[0]):
+        if p.lens[b] == 1:
+            assert not p.dq[b].any() and not p.dk[b].any() and bool(p.dv[b, 0].any())
+
+
 @pytest.mark.parametrize("dtype", [W.BF16, W.FP16], ids=["bf16", "fp16"])
 @pytest.mark.parametrize("shape", [(9, 32, 1500, 1, 1, 64), (9, 3, 1500, 8, 1, 128), (9, 1, 140, 40, 40, 128), (9, 7, 161, 8, 2, 64)], ids=lambda s: "x".join(map(str, s)))
 def test_gradients_of_few_rows(shape, dtype):
